@@ -405,6 +405,183 @@ int nuna_chain_create(const void* const* src_sets, void* const* dst_sets, int ns
 int nuna_chain_launch(void* chain, void* stream);      /* one replay of all nodes, asynchronous on `stream` */
 int nuna_chain_destroy(void* chain);
 
+/* ---- operators around the collectives --------------------------------------------------------------------
+ * What a tensor-parallel program does next to its collectives, each with its gradient: the embedding lookup
+ * over a slice of the vocabulary, whose partial rows an allreduce adds up; the layer norm, with the residual
+ * added, that follows every allreduce; tokens sorted by expert, which an alltoall carries, and their way back
+ * with the router's weights.  One rank's call each: single buffers instead of tables of rank buffers.
+ *
+ * Conventions, these entry points:
+ *  - Arguments come in a structure that is read during the call.  Buffers are device memory of the current
+ *    device, aligned to their element type (rows that are 16-byte aligned and a whole number of 16-byte vectors
+ *    long are faster).  An optional pointer is NULL where it is not wanted.
+ *  - Matrices are rows of `hidden` contiguous elements; *_stride is the distance between rows in elements (at
+ *    least `hidden`; 0 = `hidden`).  What lies between the rows is neither read nor written.
+ *  - Calls are asynchronous on `stream` and allocate nothing; workspaces belong to the caller (two calls that may
+ *    overlap, captured graphs among them, need two), and the first call on a device may be a captured one.
+ *    `flags`: NUNA_LAUNCH_PDL and, where said, NUNA_GRAD_ACCUMULATE.
+ *  - No written range may overlap another range of the call (NUNA_ERR_ALIAS) but where said; a range reaches from
+ *    a matrix's first byte to its last, the gaps between rows included.
+ *  - Sizes are at most 2^31 - 1 rows, tokens, table rows, pairs or elements in a row, and 2^46 bytes a matrix
+ *    (NUNA_ERR_TOO_LARGE).  Sizes of zero are valid: outputs that a sum over nothing defines are written.
+ *  - Arithmetic is binary32 whatever the element type, in an order that sizes and types alone decide, with one
+ *    rounding at the end: the same call gives the same bits.                                                  */
+
+/* `flags`, bit 15: gradients of parameters (dweight, dbias, dtable) are added to what their buffers hold (in
+ * binary32, rounded once) instead of replacing it.                                                           */
+#define NUNA_GRAD_ACCUMULATE  32768u
+
+/* Layer norm of each row.  With `residual`, the rows are s = rne(x + residual), stored to `summed` (which then
+ * must be given, and may be `residual` itself, with the same stride); without it s = x and `summed` must be NULL.
+ *   mean = sum(s) / hidden,  rstd = 1 / sqrt(sum((s - mean)^2) / hidden + eps),
+ *   y = rne((s - mean) * rstd * weight + bias).
+ * `weight` / `bias` (NULL: ones / zeros) are [hidden] of param_dtype: dtype or NUNA_F32.  mean, rstd: optional
+ * [rows], what the backward pass takes.                                                                      */
+typedef struct nuna_layernorm {
+    size_t rows, hidden;
+    const void* x;
+    const void* residual;
+    const void* weight;
+    const void* bias;
+    void* summed;
+    void* y;
+    float* mean;
+    float* rstd;
+    size_t x_stride, residual_stride, summed_stride, y_stride;
+    float eps;                   /* >= 0 */
+    int dtype, param_dtype;
+} nuna_layernorm_t;
+int nuna_layernorm_forward(const nuna_layernorm_t* args, unsigned flags, void* stream);
+
+/* Gradient of the layer norm.  x: the rows s that were normalised; xh = (x - mean) * rstd; g = dy * weight:
+ *   dx = rne(rstd * (g - sum(g)/hidden - xh * sum(g * xh)/hidden) + dsummed),
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy   (param_dtype; either may be NULL).
+ * dsummed: optional, the gradient that reaches s past the norm; dx is then the gradient of both x and residual, and
+ * may be `dsummed` itself, with the same stride.  workspace: nuna_layernorm_workspace bytes, 16-byte aligned,
+ * needed if dweight or dbias is given.  flags: NUNA_GRAD_ACCUMULATE.                                         */
+typedef struct nuna_layernorm_grad {
+    size_t rows, hidden;
+    const void* dy;
+    const void* x;
+    const float* mean;
+    const float* rstd;
+    const void* weight;
+    const void* dsummed;
+    void* dx;
+    void* dweight;
+    void* dbias;
+    void* workspace;
+    size_t workspace_bytes;
+    size_t dy_stride, x_stride, dsummed_stride, dx_stride;
+    int dtype, param_dtype;
+} nuna_layernorm_grad_t;
+int nuna_layernorm_backward(const nuna_layernorm_grad_t* args, unsigned flags, void* stream);
+size_t nuna_layernorm_workspace(size_t rows, size_t hidden);
+
+/* Embedding lookup over the rows [vocab_start, vocab_start + vocab_rows) of a vocabulary, which `table` holds:
+ *   out[t] = rne(scale * table[ids[t] - vocab_start]), a row of zeros for an id outside of them (negative ones
+ * too): the sum over ranks that hold the other rows is the whole lookup.  ids: int32 or int64 (id_bytes 4, 8). */
+typedef struct nuna_embedding {
+    size_t tokens, hidden, vocab_rows;
+    const void* ids;
+    const void* table;
+    void* out;
+    size_t table_stride, out_stride;
+    long long vocab_start;
+    float scale;
+    int id_bytes, dtype;
+} nuna_embedding_t;
+int nuna_embedding_forward(const nuna_embedding_t* args, unsigned flags, void* stream);
+
+/* Gradient of the lookup: dtable[v] = rne(scale * sum of dout[t] over the tokens with ids[t] = vocab_start + v);
+ * every row is written, rows without a token with zeros.  With NUNA_GRAD_ACCUMULATE the sum is added to
+ * dtable[v], and rows without a token are neither read nor written.  grad_dtype (of dtable): dtype or NUNA_F32.
+ * The tokens are sorted by id first, so the sum's order is fixed.  workspace: nuna_embedding_workspace bytes,
+ * 16-byte aligned.                                                                                           */
+typedef struct nuna_embedding_grad {
+    size_t tokens, hidden, vocab_rows;
+    const void* ids;
+    const void* dout;
+    void* dtable;
+    void* workspace;
+    size_t workspace_bytes;
+    size_t dout_stride, dtable_stride;
+    long long vocab_start;
+    float scale;
+    int id_bytes, dtype, grad_dtype;
+} nuna_embedding_grad_t;
+int nuna_embedding_backward(const nuna_embedding_grad_t* args, unsigned flags, void* stream);
+size_t nuna_embedding_workspace(size_t tokens, size_t hidden, size_t vocab_rows);
+
+/* Sorts the (token, choice) pairs p = t * topk + j by expert, pairs of one expert in their own order.  experts:
+ * [tokens][topk] int32 or int64; those outside [first_expert, first_expert + num_experts) are another rank's (or
+ * nobody's) and dropped.  num_experts <= NUNA_MAX_EXPERTS, tokens * topk < 2^31.
+ *   capacity == 0: packed.  Expert e's pairs take the rows offsets[e] ... offsets[e+1] - 1; there are tokens * topk
+ *                  rows, of which the last ones stay unused if pairs were dropped.
+ *   capacity  > 0: every expert has `capacity` rows from offsets[e] = e * capacity on (num_experts * capacity rows in
+ *                  all: equal blocks for nuna_alltoall); its pairs beyond that are dropped.
+ * row_of_pair [tokens * topk]: each pair's row, -1 if dropped.  pair_of_row [rows]: each row's pair, -1 if it has
+ * none.  offsets [num_experts + 1].  counts [num_experts], optional: pairs that asked for the expert, dropped ones
+ * included.  All int32.                                                                                      */
+#define NUNA_MAX_EXPERTS 1024
+typedef struct nuna_expert_sort {
+    size_t tokens, topk, num_experts, capacity;
+    const void* experts;
+    int* row_of_pair;
+    int* pair_of_row;
+    int* offsets;
+    int* counts;
+    long long first_expert;
+    int id_bytes;
+} nuna_expert_sort_t;
+int nuna_expert_sort(const nuna_expert_sort_t* args, unsigned flags, void* stream);
+
+/* out[row_of_pair[t * topk + j]] = x[t], bit for bit.  With pair_of_row, rows whose entry is -1 are zeroed (what an
+ * alltoall sends); without it rows that no pair has stay as they are.  rows: rows of `out`; an entry of row_of_pair
+ * outside [0, rows) is a dropped pair here and below.                                                         */
+typedef struct nuna_expert_dispatch {
+    size_t tokens, topk, rows, hidden;
+    const void* x;
+    const int* row_of_pair;
+    const int* pair_of_row;
+    void* out;
+    size_t x_stride, out_stride;
+    int dtype;
+} nuna_expert_dispatch_t;
+int nuna_expert_dispatch(const nuna_expert_dispatch_t* args, unsigned flags, void* stream);
+
+/* y[t] = rne(sum over j, ascending, of weights[t * topk + j] * src[row_of_pair[t * topk + j]]), dropped pairs skipped
+ * (their weights are not looked at); a token without any gets zeros.  weights: [tokens][topk] binary32, or NULL for
+ * ones, which makes it the gradient of nuna_expert_dispatch.                                                  */
+typedef struct nuna_expert_combine {
+    size_t tokens, topk, rows, hidden;
+    const void* src;
+    const int* row_of_pair;
+    const float* weights;
+    void* y;
+    size_t src_stride, y_stride;
+    int dtype;
+} nuna_expert_combine_t;
+int nuna_expert_combine(const nuna_expert_combine_t* args, unsigned flags, void* stream);
+
+/* Gradient of the weighted nuna_expert_combine: for every kept pair p of token t with row r,
+ *   dsrc[r] = rne(weights[p] * dy[t]),  dweights[p] = sum over the row of dy[t] * src[r]  (0 for a dropped pair).
+ * dweights may be NULL (src is then not read).  With pair_of_row, rows of dsrc whose entry is -1 are zeroed; without
+ * it they stay as they are.                                                                                    */
+typedef struct nuna_expert_combine_grad {
+    size_t tokens, topk, rows, hidden;
+    const void* dy;
+    const void* src;
+    const float* weights;
+    const int* row_of_pair;
+    const int* pair_of_row;
+    void* dsrc;
+    float* dweights;
+    size_t dy_stride, src_stride, dsrc_stride;
+    int dtype;
+} nuna_expert_combine_grad_t;
+int nuna_expert_combine_backward(const nuna_expert_combine_grad_t* args, unsigned flags, void* stream);
+
 /* Reads and clears the device status of the current device (NUNA_OK or NUNA_ERR_TIMEOUT) after
  * synchronising the device: the worse of the context's status word and the allocation-free entry
  * point's.  After a timeout the control words are rewound (the epoch keeps counting).                  */

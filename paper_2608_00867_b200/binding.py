@@ -41,6 +41,8 @@ NUNA_CHAIN_PERSISTENT = 2048
 NUNA_CHAIN_GRAPH = 4096
 NUNA_TWOSHOT_SYS_SCOPE = 8192
 NUNA_PLACE_REGS = 16384
+NUNA_GRAD_ACCUMULATE = 32768
+NUNA_MAX_EXPERTS = 1024
 
 NUNA_MAX_SMS, NUNA_MAX_PROBE_BUFS, NUNA_PROBE_REGIONS, NUNA_MAX_PROBE_LINES = 256, 32, 8, 2048
 NUNA_TOPO_UNIFORM, NUNA_TOPO_NONUNIFORM = 0, 1
@@ -169,6 +171,9 @@ def lib() -> ctypes.CDLL:
         L.nuna_debug_launch_floor.restype = ctypes.c_int
         L.nuna_debug_twoshot.argtypes = [vpp, vpp, ctypes.c_int, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint, ctypes.c_uint]
         L.nuna_debug_twoshot.restype = ctypes.c_int
+        for name, sizes in (("nuna_layernorm_workspace", 2), ("nuna_embedding_workspace", 3)):
+            getattr(L, name).argtypes = [ctypes.c_size_t] * sizes
+            getattr(L, name).restype = ctypes.c_size_t
         _lib = L
     return _lib
 
@@ -187,6 +192,9 @@ def ptr_table(bufs: Sequence):
 # The collectives the native module is pointed at, in its order.
 _COLLECTIVES = ("nuna_allreduce", "nuna_allreduce_oneshot", "nuna_allreduce_twoshot", "nuna_reduce_scatter", "nuna_allgather",
                 "nuna_alltoall")
+# The operators around them, likewise.
+_OPERATORS = ("nuna_layernorm_forward", "nuna_layernorm_backward", "nuna_embedding_forward", "nuna_embedding_backward",
+              "nuna_expert_sort", "nuna_expert_dispatch", "nuna_expert_combine", "nuna_expert_combine_backward")
 _native = None
 
 
@@ -206,6 +214,7 @@ def _load_native():
         spec.loader.exec_module(m)
         at = lambda name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value
         m.bind(tuple(at(n) for n in _COLLECTIVES), at("nuna_allreduce_twoshot_static"), at("nuna_allreduce_host"), NunaError)
+        m.bind_operators(tuple(at(n) for n in _OPERATORS))
         for name, stand_in in _STAND_INS.items():
             if globals()[name] is stand_in:
                 globals()[name] = getattr(m, name)
@@ -269,8 +278,83 @@ def nuna_allreduce_host(src, dst, count, dtype=NUNA_BF16, flags=0, two_shot=Fals
     return _load_native().nuna_allreduce_host(src, dst, count, dtype, flags, two_shot, check)
 
 
+# ---- operators around the collectives (include/nuna.h says what they compute).  Buffers are CUDA tensors of the current device
+# or addresses; a tensor whose storage is shorter than the call's sizes and strides reach is refused (NUNA_ERR_INVALID_ARG).
+# Strides are in elements, 0 for rows without gaps; workspaces are the caller's, any tensor of at least nuna_*_workspace() bytes.
+
+def nuna_layernorm_forward(x, y, rows, hidden, weight=None, bias=None, residual=None, summed=None, mean=None, rstd=None, eps=1e-5,
+                           dtype=NUNA_BF16, param_dtype=NUNA_BF16, x_stride=0, residual_stride=0, summed_stride=0, y_stride=0,
+                           flags=0, stream=None, check=True) -> int:
+    """Layer norm of each row of ``x`` (with ``residual``: of ``summed`` = x + residual) into ``y``."""
+    return _load_native().nuna_layernorm_forward(x, y, rows, hidden, weight, bias, residual, summed, mean, rstd, eps, dtype, param_dtype,
+                                                 x_stride, residual_stride, summed_stride, y_stride, flags, stream, check)
+
+
+def nuna_layernorm_backward(dy, x, mean, rstd, dx, rows, hidden, weight=None, dsummed=None, dweight=None, dbias=None, workspace=None,
+                            dtype=NUNA_BF16, param_dtype=NUNA_BF16, dy_stride=0, x_stride=0, dsummed_stride=0, dx_stride=0,
+                            workspace_bytes=None, flags=0, stream=None, check=True) -> int:
+    """Gradient of the layer norm.  ``workspace_bytes`` only for a workspace given by its address."""
+    kw = {} if workspace_bytes is None else {"workspace_bytes": workspace_bytes}
+    return _load_native().nuna_layernorm_backward(dy, x, mean, rstd, dx, rows, hidden, weight, dsummed, dweight, dbias, workspace, dtype,
+                                                  param_dtype, dy_stride, x_stride, dsummed_stride, dx_stride, flags=flags, stream=stream,
+                                                  check=check, **kw)
+
+
+def nuna_layernorm_workspace(rows: int, hidden: int) -> int:
+    return lib().nuna_layernorm_workspace(rows, hidden)
+
+
+def nuna_embedding_forward(ids, table, out, tokens, hidden, vocab_rows, vocab_start=0, scale=1.0, dtype=NUNA_BF16, id_bytes=8,
+                           table_stride=0, out_stride=0, flags=0, stream=None, check=True) -> int:
+    """Rows ``ids - vocab_start`` of ``table``, scaled; zeros for ids outside of its ``vocab_rows`` rows."""
+    return _load_native().nuna_embedding_forward(ids, table, out, tokens, hidden, vocab_rows, vocab_start, scale, dtype, id_bytes,
+                                                 table_stride, out_stride, flags, stream, check)
+
+
+def nuna_embedding_backward(ids, dout, dtable, tokens, hidden, vocab_rows, workspace=None, vocab_start=0, scale=1.0, dtype=NUNA_BF16,
+                            grad_dtype=NUNA_BF16, id_bytes=8, dout_stride=0, dtable_stride=0, workspace_bytes=None,
+                            flags=0, stream=None, check=True) -> int:
+    """Gradient of the lookup, dense (or added to ``dtable`` with NUNA_GRAD_ACCUMULATE)."""
+    kw = {} if workspace_bytes is None else {"workspace_bytes": workspace_bytes}
+    return _load_native().nuna_embedding_backward(ids, dout, dtable, tokens, hidden, vocab_rows, workspace, vocab_start, scale, dtype,
+                                                  grad_dtype, id_bytes, dout_stride, dtable_stride, flags=flags, stream=stream,
+                                                  check=check, **kw)
+
+
+def nuna_embedding_workspace(tokens: int, hidden: int, vocab_rows: int) -> int:
+    return lib().nuna_embedding_workspace(tokens, hidden, vocab_rows)
+
+
+def nuna_expert_sort(experts, row_of_pair, pair_of_row, offsets, tokens, topk, num_experts, counts=None, first_expert=0, capacity=0,
+                     id_bytes=8, flags=0, stream=None, check=True) -> int:
+    """Rows of the (token, choice) pairs sorted by expert, packed or with ``capacity`` rows each."""
+    return _load_native().nuna_expert_sort(experts, row_of_pair, pair_of_row, offsets, tokens, topk, num_experts, counts, first_expert,
+                                           capacity, id_bytes, flags, stream, check)
+
+
+def nuna_expert_dispatch(x, row_of_pair, out, tokens, topk, rows, hidden, pair_of_row=None, dtype=NUNA_BF16, x_stride=0, out_stride=0,
+                         flags=0, stream=None, check=True) -> int:
+    """Every token's row to the rows of its pairs; with ``pair_of_row``, rows without a pair are zeroed."""
+    return _load_native().nuna_expert_dispatch(x, row_of_pair, out, tokens, topk, rows, hidden, pair_of_row, dtype, x_stride, out_stride,
+                                               flags, stream, check)
+
+
+def nuna_expert_combine(src, row_of_pair, y, tokens, topk, rows, hidden, weights=None, dtype=NUNA_BF16, src_stride=0, y_stride=0,
+                        flags=0, stream=None, check=True) -> int:
+    """The (weighted) sum of the rows of every token's pairs."""
+    return _load_native().nuna_expert_combine(src, row_of_pair, y, tokens, topk, rows, hidden, weights, dtype, src_stride, y_stride,
+                                              flags, stream, check)
+
+
+def nuna_expert_combine_backward(dy, src, weights, row_of_pair, dsrc, dweights, tokens, topk, rows, hidden, pair_of_row=None,
+                                 dtype=NUNA_BF16, dy_stride=0, src_stride=0, dsrc_stride=0, flags=0, stream=None, check=True) -> int:
+    """Gradients of the weighted nuna_expert_combine."""
+    return _load_native().nuna_expert_combine_backward(dy, src, weights, row_of_pair, dsrc, dweights, tokens, topk, rows, hidden,
+                                                       pair_of_row, dtype, dy_stride, src_stride, dsrc_stride, flags, stream, check)
+
+
 # This module's own functions that _load_native replaces.
-_STAND_INS = {name: globals()[name] for name in _COLLECTIVES + ("nuna_allreduce_twoshot_static", "nuna_allreduce_host")}
+_STAND_INS = {name: globals()[name] for name in _COLLECTIVES + _OPERATORS + ("nuna_allreduce_twoshot_static", "nuna_allreduce_host")}
 
 
 def nuna_chain_create(src_sets, dst_sets, nnodes, count, dtype=NUNA_BF16, flags=0, two_shot=False, check=True):

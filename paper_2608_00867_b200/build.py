@@ -13,7 +13,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnuna.so")
-NATIVE_SRC = os.path.join(CSRC, "python", "nuna_py.cpp")
+NATIVE_SRC = [os.path.join(CSRC, "python", name) for name in ("nuna_py.cpp", "nuna_py_ops.cpp")]
+NATIVE_HEADERS = [os.path.join(CSRC, "python", "nuna_py.h"), os.path.join(CSRC, "nuna_spans.h")]
 
 
 def _torch_version() -> str:
@@ -69,7 +70,7 @@ def _compile(cmd, target: str, verbose: bool) -> None:
 def build_native(force: bool = False, verbose: bool = False) -> str:
     """The marshalling module: reads addresses and the current stream out of torch's own objects."""
     target = native_path()
-    if not force and not _older(target, [NATIVE_SRC] + _public_headers()):
+    if not force and not _older(target, NATIVE_SRC + NATIVE_HEADERS + _public_headers()):
         return target
     torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
     inc = os.path.join(torch_dir, "include")
@@ -77,7 +78,7 @@ def build_native(force: bool = False, verbose: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall", "-shared", "-I" + sysconfig.get_paths()["include"]]
     for d in (inc, os.path.join(inc, "torch", "csrc", "api", "include"), os.path.join(cuda, "include")):
         cmd += ["-isystem", d]
-    cmd += [NATIVE_SRC, "-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
+    cmd += NATIVE_SRC + ["-L" + os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda"]
     _compile(cmd, target, verbose)
     return target
 

@@ -259,7 +259,7 @@ static unsigned launch_mode(unsigned flags, size_t total_src_bytes = 0)
 // prefetch ahead of the wait pays as it does with the flag (8 x 4 MiB flag two-shot: 15.6 -> 14.2 us).  While a stream
 // is captured the caller's choice stands: the graph has the edges it asked for.  (The legacy default stream cannot be
 // captured, and must not be asked about while another stream is.)
-static unsigned effective_flags(unsigned flags, void* stream)
+unsigned effective_flags(unsigned flags, void* stream)
 {
     if (flags & NUNA_LAUNCH_PDL) return flags;
     const cudaStream_t s = (cudaStream_t)stream;

@@ -83,6 +83,7 @@ int check_args(const void* const* src, void* const* dst, int nranks, size_t src_
 void plan_oneshot_lists(const nuna_topology_t* topo, int num_sms, int nranks, size_t ntiles, size_t tile_bytes,
                         bool generic, int domains, std::vector<std::vector<unsigned>>& lists);
 size_t elem_size(int dtype);
+unsigned effective_flags(unsigned flags, void* stream);
 int prepare_oneshot(Context* c, int nranks, int dtype, size_t count, unsigned flags);
 int launch_oneshot(Context* c, const RankPtrs& p, int nranks, int dtype, size_t count, unsigned flags, cudaStream_t stream);
 int launch_twoshot(Context* c, const RankPtrs& p, int nranks, int dtype, size_t count, unsigned flags, cudaStream_t stream);

@@ -17,9 +17,9 @@
 #include <memory>
 #include <new>
 
-#include "../../../include/nuna.h"
+#include "nuna_py.h"
 
-namespace {
+namespace nuna_py {
 
 typedef int (*CollectiveFn)(const void* const*, void* const*, int, size_t, int, unsigned, void*);
 typedef int (*StaticFn)(const void* const*, void* const*, int, size_t, int, void*);
@@ -327,7 +327,9 @@ PyMethodDef methods[] = {
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_nuna_py", "Marshalling of the nuna C ABI's calls.", -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
-}  // namespace
+}  // namespace nuna_py
+
+using namespace nuna_py;
 
 PyMODINIT_FUNC PyInit__nuna_py()
 {
@@ -337,5 +339,10 @@ PyMODINIT_FUNC PyInit__nuna_py()
     g_s_data = PyUnicode_InternFromString("data");
     for (Signature* sig : {&g_count, &g_shard, &g_block, &g_fixed, &g_hosts})
         for (int i = 0; i < sig->n; ++i) sig->name[i] = PyUnicode_InternFromString(sig->text[i]);
-    return PyModule_Create(&module_def);
+    PyObject* m = PyModule_Create(&module_def);
+    if (m && !add_operators(m)) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
 }

@@ -1,0 +1,132 @@
+"""A layer's path through the operators and the collectives, as eight emulated ranks of a tensor-parallel program run it: vocabulary
+slices looked up and added by an allreduce, residual and norm, tokens to their experts by alltoall and back, and the way back with the
+gradients, against the same path in 64 bits."""
+import pytest
+import torch
+
+from operator_cases import U, generator, half_step, integers, normal, within
+from paper_2608_00867_b200 import binding as nb
+
+pytestmark = pytest.mark.gpu
+
+RANKS, TOKENS, HIDDEN, VOCAB, EXPERTS, TOPK, CAPACITY = 8, 24, 512, 80, 16, 2, 6
+F32 = dict(dtype=nb.NUNA_F32)
+
+
+def zeros(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+
+@pytest.mark.parametrize("flags", [0, nb.NUNA_LAUNCH_PDL])
+@pytest.mark.parametrize("graph", [False, True])
+def test_lookup_allreduce_norm_and_back(flags, graph):
+    """Each rank holds a tenth of the vocabulary; ranks 0 ... 7 cover all of it."""
+    gen = generator(1)
+    per = VOCAB // RANKS
+    ids = torch.randint(0, VOCAB, (TOKENS,), generator=gen, device="cuda")
+    table, residual, up = normal(gen, VOCAB, HIDDEN), normal(gen, TOKENS, HIDDEN), normal(gen, TOKENS, HIDDEN)
+    w, b = 1 + 0.1 * normal(gen, HIDDEN), normal(gen, HIDDEN)
+    slices = [table[r * per:(r + 1) * per].contiguous() for r in range(RANKS)]
+    part, whole = [zeros(TOKENS, HIDDEN) for _ in range(RANKS)], [zeros(TOKENS, HIDDEN) for _ in range(RANKS)]
+    summed, y, mean, rstd, dx = zeros(TOKENS, HIDDEN), zeros(TOKENS, HIDDEN), zeros(TOKENS), zeros(TOKENS), zeros(TOKENS, HIDDEN)
+    dw, db, grads = zeros(HIDDEN), zeros(HIDDEN), [zeros(per, HIDDEN) for _ in range(RANKS)]
+    ws = zeros(nb.nuna_layernorm_workspace(TOKENS, HIDDEN), dtype=torch.uint8)
+    ews = [zeros(nb.nuna_embedding_workspace(TOKENS, HIDDEN, per), dtype=torch.uint8) for _ in range(RANKS)]
+
+    def step():
+        for r in range(RANKS):
+            nb.nuna_embedding_forward(ids, slices[r], part[r], TOKENS, HIDDEN, per, vocab_start=r * per, scale=2.0, flags=flags, **F32)
+        nb.nuna_allreduce(part, whole, TOKENS * HIDDEN, flags=flags | nb.NUNA_PLACE_AUTO, **F32)
+        nb.nuna_layernorm_forward(whole[3], y, TOKENS, HIDDEN, weight=w, bias=b, residual=residual, summed=summed, mean=mean, rstd=rstd,
+                                  param_dtype=nb.NUNA_F32, flags=flags, **F32)
+        nb.nuna_layernorm_backward(up, summed, mean, rstd, dx, TOKENS, HIDDEN, weight=w, dsummed=y, dweight=dw, dbias=db, workspace=ws,
+                                   param_dtype=nb.NUNA_F32, flags=flags, **F32)
+        for r in range(RANKS):
+            nb.nuna_embedding_backward(ids, dx, grads[r], TOKENS, HIDDEN, per, workspace=ews[r], vocab_start=r * per, scale=2.0,
+                                       grad_dtype=nb.NUNA_F32, flags=flags, **F32)
+
+    if graph:
+        nb.nuna_init(4 * TOKENS * HIDDEN)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        g.replay()
+        g.replay()
+    else:
+        step()
+        step()
+    torch.cuda.synchronize()
+    for r in range(RANKS):
+        assert torch.equal(whole[r], table[ids] * 2.0)                 # one rank's row and seven zeros
+    s = (whole[3] + residual).double()
+    assert torch.equal(summed.double(), s)
+    x = s.clone().requires_grad_()
+    w64, b64 = w.double().requires_grad_(), b.double().requires_grad_()
+    xh = (x - x.mean(-1, keepdim=True)) * (x.var(-1, unbiased=False, keepdim=True) + 1e-5).rsqrt()
+    out = xh * w64 + b64
+    # 42 additions in a row at most (32 and 10 levels) of values near 1, a handful of roundings, doubled; xh and the weights are below 8
+    within(y, out.detach(), torch.full_like(out.detach(), 2 * 64 * 8 * U), "y")
+    (out * up.double()).sum().backward()
+    want = x.grad + y.double()
+    within(dx, want, torch.full_like(want, 2 * 64 * 32 * U), "dx")
+    within(dw, w64.grad, torch.full_like(dw.double(), 2 * 64 * TOKENS * 16 * U), "dweight")
+    within(db, b64.grad, torch.full_like(db.double(), 2 * TOKENS * TOKENS * 4 * U), "dbias")
+    want = torch.zeros(VOCAB, HIDDEN, dtype=torch.float64, device="cuda").index_add_(0, ids, dx.double()) * 2.0
+    within(torch.cat(grads), want, TOKENS * U * 2 * torch.zeros_like(want).index_add_(0, ids, dx.double().abs()), "dtable")
+    assert nb.nuna_device_status() == nb.NUNA_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_to_experts_on_other_ranks_and_back(dtype):
+    """Every rank sorts its own tokens into equal blocks, an alltoall carries them to the experts' ranks and back.  Integers and
+    weights of one half: exact throughout, dropped pairs included."""
+    tdt, code = {"bf16": (torch.bfloat16, nb.NUNA_BF16), "f32": (torch.float32, nb.NUNA_F32)}[dtype]
+    rows, per = EXPERTS * CAPACITY, EXPERTS // RANKS
+    block = per * CAPACITY * HIDDEN
+    gens = [generator(2, r) for r in range(RANKS)]
+    ids = [torch.stack([torch.randperm(EXPERTS, generator=g, device="cuda")[:TOPK] for _ in range(TOKENS)]) for g in gens]
+    x = [integers(g, -3, 3, TOKENS, HIDDEN).to(tdt) for g in gens]
+    up = [integers(g, -1, 1, TOKENS, HIDDEN).to(tdt) for g in gens]
+    weights = [torch.full((TOKENS, TOPK), 0.5, device="cuda") for _ in gens]
+    ints = lambda n: [zeros(n, dtype=torch.int32) for _ in gens]
+    row, pair, offsets, counts = ints(TOKENS * TOPK), ints(rows), ints(EXPERTS + 1), ints(EXPERTS)
+    many = lambda: [torch.full((rows, HIDDEN), float("nan"), dtype=tdt, device="cuda") for _ in gens]
+    send, arrived, back, y = many(), many(), many(), [zeros(TOKENS, HIDDEN, dtype=tdt) for _ in gens]
+    factor = torch.arange(1, EXPERTS + 1, device="cuda") % 4 + 1       # expert e multiplies by e % 4 + 1
+    for r in range(RANKS):
+        nb.nuna_expert_sort(ids[r], row[r], pair[r], offsets[r], TOKENS, TOPK, EXPERTS, counts=counts[r], capacity=CAPACITY)
+        nb.nuna_expert_dispatch(x[r], row[r], send[r], TOKENS, TOPK, rows, HIDDEN, pair_of_row=pair[r], dtype=code)
+    nb.nuna_alltoall(send, arrived, block, dtype=code)
+    own = lambda r: factor[r * per:(r + 1) * per].repeat_interleave(CAPACITY).repeat(RANKS)[:, None]
+    made = [(arrived[r] * own(r)).to(tdt) for r in range(RANKS)]
+    nb.nuna_alltoall(made, back, block, dtype=code)
+    dsrc, dweights, dmade, dout, dx = many(), [zeros(TOKENS, TOPK) for _ in gens], many(), many(), [zeros(TOKENS, HIDDEN, dtype=tdt) for _ in gens]
+    for r in range(RANKS):
+        nb.nuna_expert_combine(back[r], row[r], y[r], TOKENS, TOPK, rows, HIDDEN, weights=weights[r], dtype=code)
+        nb.nuna_expert_combine_backward(up[r], back[r], weights[r], row[r], dsrc[r], dweights[r], TOKENS, TOPK, rows, HIDDEN,
+                                        pair_of_row=pair[r], dtype=code)
+    nb.nuna_alltoall(dsrc, dmade, block, dtype=code)
+    darrived = [(dmade[r] * own(r)).to(tdt) for r in range(RANKS)]
+    nb.nuna_alltoall(darrived, dout, block, dtype=code)
+    for r in range(RANKS):
+        nb.nuna_expert_combine(dout[r], row[r], dx[r], TOKENS, TOPK, rows, HIDDEN, dtype=code)
+    torch.cuda.synchronize()
+    dropped = 0
+    for r in range(RANKS):
+        kept = torch.zeros(TOKENS, TOPK, dtype=torch.float64, device="cuda")
+        seen = [0] * EXPERTS
+        for t, choices in enumerate(ids[r].tolist()):
+            for j, e in enumerate(choices):
+                kept[t, j] = float(seen[e] < CAPACITY)
+                seen[e] += 1
+        assert counts[r].tolist() == seen
+        dropped += int((kept == 0).sum())
+        f = factor.double()[ids[r]] * kept
+        assert torch.equal(y[r].double(), (f.sum(1) * 0.5)[:, None] * x[r].double())
+        assert torch.equal(dx[r].double(), (f.sum(1) * 0.5)[:, None] * up[r].double())
+        assert torch.equal(dweights[r].double(), f * (x[r].double() * up[r].double()).sum(1)[:, None])
+        for e in range(EXPERTS):                                       # empty rows were sent as zeros
+            n = min(seen[e], CAPACITY)
+            assert bool((send[r][e * CAPACITY + n:(e + 1) * CAPACITY] == 0).all())
+    assert dropped > 0
+    assert half_step(tdt) > 0 and nb.nuna_device_status() == nb.NUNA_OK

@@ -35,21 +35,6 @@ constexpr int min_blocks(int vectors)
 
 // ---- the fold ------------------------------------------------------------------------------
 
-// bf16 -> binary32 is a 16-bit shift; a 32-bit word holds element 2k in its low half and 2k+1 in
-// its high half.  Rank 0's value is widened (shift / mask for bf16, cvt for f16); ranks 1..N-1 are
-// folded in with the sm_100 mixed-precision add, d = f32(a) + c rounded once to binary32 (nearest
-// even, subnormals kept), so no instruction is spent on widening them.  At large sizes the one-shot is
-// limited by instruction issue and L1 throughput (N times the work of a plain sum), which is why the
-// instruction count matters.
-template <int DT>
-__device__ __forceinline__ float add_narrow(float acc, uint16_t h)
-{
-    float d;
-    if (DT == kBf16) asm("add.rn.f32.bf16 %0, %1, %2;" : "=f"(d) : "h"(h), "f"(acc));
-    else             asm("add.rn.f32.f16 %0, %1, %2;" : "=f"(d) : "h"(h), "f"(acc));
-    return d;
-}
-
 template <int DT>
 __device__ __forceinline__ void fold_word(float& lo, float& hi, uint32_t w)
 {

@@ -16,7 +16,7 @@ struct NormArgs {
     float *mean, *rstd;
     size_t x_stride, residual_stride, summed_stride, y_stride;       // bytes
     unsigned rows, hidden, packs, group;                             // packs in a row, threads of a group
-    float eps, count;                                                // count: hidden
+    float eps, count, inverse;                                       // count: hidden; inverse: 1 / hidden
 };
 
 struct NormGradArgs {
@@ -26,143 +26,259 @@ struct NormGradArgs {
     float* part;                                                     // [gridDim.x][2][part_stride], or null
     size_t dy_stride, x_stride, dsummed_stride, dx_stride;           // bytes
     unsigned rows, hidden, packs, group, part_stride;
-    float count;                                                     // hidden
+    float count, inverse;                                            // hidden, 1 / hidden
 };
 
-// Sums v over the `warps` warps of this thread's group, for every group of the block at once (all threads call).  Two
-// consecutive calls use different halves of `red`, [2][32][N]: the exchange of the second separates the uses of the first.
+// Sums v over the warps of this thread's group (all threads of the group call; g: the group's number in its block).  Groups
+// do not wait for one another.  Two consecutive calls use different halves of `red`, [2][32][N]: the exchange of the second
+// separates the uses of the first.
 template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], unsigned warps, float* red)
+__device__ __forceinline__ void group_sum(float (&v)[N], unsigned warps, unsigned g, float* red)
 {
     warp_sum<N>(v);
     if (warps == 1u) return;
-    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, first = warp / warps * warps;
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, first = g * warps;
     if (lane == 0u)
 #pragma unroll
         for (int i = 0; i < N; ++i) red[warp * N + i] = v[i];
-    __syncthreads();
+    asm volatile("bar.sync %0, %1;" :: "r"(1u + g), "r"(warps * 32u) : "memory");
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = lane < warps ? red[(first + lane) * N + i] : 0.0f;
     warp_sum<N>(v);
 }
 
+// sum / count.  The reciprocal's rounding is taken back by the remainder, so that equal elements have themselves as their mean.
+__device__ __forceinline__ float quotient(float sum, float count, float inverse)
+{
+    const float q = sum * inverse;
+    const float better = fmaf(fmaf(-q, count, sum), inverse, q);
+    return isfinite(q) ? better : q;
+}
+
+// The rows that a group takes, one after the other, fetched ahead of their use.  Vectors go through shared memory by
+// asynchronous copies: a thread fetches, kDepth rows ahead, just the vectors that it will use, so it waits for its own copies
+// only, and what is in flight holds no registers.  Single elements are loaded into registers, a row ahead where there are
+// enough of them.
+template <int DT, int kPacks, bool kVec, int kStreams, int kDepth>
+struct RowFetch {
+    const void* from[kStreams];
+    size_t stride[kStreams];
+    bool given[kStreams];
+    unsigned rows, packs, group, lane;
+    uint32_t slots;                                                  // this thread's part of the shared memory: one slot per fetch
+    Pack<DT, kVec> next[kVec ? 1 : kStreams][kVec ? 1 : kPacks];
+
+    static constexpr unsigned kSlots = kVec ? kDepth * kStreams * kPacks : 0;       // 16 bytes each, per thread
+
+    __device__ __forceinline__ uint32_t slot(unsigned stage, int s, int k) const { return slots + ((stage * kStreams + s) * kPacks + k) * blockDim.x * 16u; }
+
+    // Starts fetching `row` as the stage-th of the ring.
+    __device__ __forceinline__ void start(unsigned long long row, unsigned stage)
+    {
+#pragma unroll
+        for (int s = 0; s < kStreams; ++s) {
+            if (!given[s]) continue;
+            const void* at = row_at(from[s], (size_t)row, stride[s]);
+#pragma unroll
+            for (int k = 0; k < kPacks; ++k) {
+                const unsigned i = lane + k * group;
+                if (row < rows && i < packs) {
+                    if constexpr (kVec) copy_async(slot(stage, s, k), static_cast<const uint4*>(at) + i);
+                    else next[s][k] = load_pack<DT, kVec>(at, i);
+                }
+            }
+        }
+        if constexpr (kVec) copy_commit();
+    }
+    __device__ __forceinline__ Pack<DT, kVec> take(unsigned stage, int s, int k) const
+    {
+        if constexpr (kVec) {
+            Pack<DT, kVec> p;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[2]), "=r"(p.w[3]) : "r"(slot(stage, s, k)));
+            return p;
+        } else {
+            return next[s][k];
+        }
+    }
+};
+
+// The parameters of a thread's columns for all of its rows: widened once where there are registers for it, or as they are stored.
+template <int PT, int E, int kPacks, bool kWide>
+struct KeptParams {
+    static constexpr int P = (E + 1) / 2;
+    Params<kWide ? kF32 : PT, E> p[kPacks];
+
+    __device__ __forceinline__ void put(int k, const Params<PT, E>& v)
+    {
+        if constexpr (kWide) {
+            float f[E];
+            unpack_params<PT, E>(f, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) p[k].w[e] = __float_as_uint(f[e]);
+        } else {
+            p[k] = v;
+        }
+    }
+    template <typename V>
+    __device__ __forceinline__ void get(V (&f)[P], int k) const
+    {
+        float v[E];
+        unpack_params<kWide ? kF32 : PT, E>(v, p[k]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) half(f[e / 2], e) = v[e];
+    }
+};
+
+// Most threads of a block, and rows that are fetched ahead of the one in work.
+__host__ __device__ constexpr int norm_threads(int packs, bool vec) { return vec && packs == 4 ? 512 : 1024; }
+__host__ __device__ constexpr int norm_depth(int packs, bool vec) { return !vec ? 2 : packs == 4 ? 2 : 3; }
+
 template <int DT, int PT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(1024) k_norm_forward(const NormArgs a)
+__global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(const NormArgs a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
+    constexpr int kDepth = norm_depth(kPacks, kVec);
     __shared__ float red[2][32];
-    pdl_wait();
+    extern __shared__ uint4 ring[];
     const unsigned warps = a.group / 32u, g = threadIdx.x / a.group, lane = threadIdx.x % a.group, groups = blockDim.x / a.group;
-    unsigned turn = 0;
-    for (unsigned long long base = (unsigned long long)blockIdx.x * groups; base < a.rows; base += (unsigned long long)gridDim.x * groups) {
-        const size_t row = base + g;
+    const unsigned long long step = (unsigned long long)gridDim.x * groups;
+    unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
+    RowFetch<DT, kPacks, kVec, 2, kDepth> fetch = {{a.x, a.residual}, {a.x_stride, a.residual_stride}, {true, a.residual != nullptr},
+                                                   a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
+    pdl_wait();
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
+    constexpr int P = kLanes<DT, kVec>;
+    using V = Lanes<kVec>;
+    KeptParams<PT, E, kPacks, (kVec && kPacks <= 2)> w, b;
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+        const unsigned i = lane + k * a.group;
+        w.put(k, load_params<PT, E>(i < a.packs ? a.weight : nullptr, i, kOne<PT>));
+        b.put(k, load_params<PT, E>(i < a.packs ? a.bias : nullptr, i, 0u));
+    }
+    unsigned turn = 0, stage = 0;
+    for (unsigned long long base = (unsigned long long)blockIdx.x * groups; base < a.rows; base += step, row += step) {
         const bool live = row < a.rows;
-        float f[kPacks][E];
+        V f[kPacks][P];
+        if constexpr (kVec) {
+            fetch.start(row + (kDepth - 1) * step, stage == 0u ? kDepth - 1 : stage - 1u);
+            copy_wait<kDepth - 1>();
+        }
+        void* to_sum = row_at(a.summed, (size_t)row, a.summed_stride);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
             const unsigned i = lane + k * a.group;
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[k][e] = 0.0f;
+            for (int e = 0; e < P; ++e) f[k][e] = all<V>(0.0f);
             if (live && i < a.packs) {
-                unpack<DT, kVec>(f[k], load_pack<DT, kVec>(row_at(a.x, row, a.x_stride), i));
+                unpack<DT, kVec>(f[k], fetch.take(stage, 0, k));
                 if (a.residual) {
-                    float r[E];
-                    unpack<DT, kVec>(r, load_pack<DT, kVec>(row_at(a.residual, row, a.residual_stride), i));
-#pragma unroll
-                    for (int e = 0; e < E; ++e) f[k][e] = __fadd_rn(f[k][e], r[e]);
+                    add_pack<DT, kVec>(f[k], fetch.take(stage, 1, k));
                     const Pack<DT, kVec> s = pack<DT, kVec>(f[k]);
-                    store_pack<DT, kVec>(row_at(a.summed, row, a.summed_stride), i, s);
+                    store_pack<DT, kVec>(to_sum, i, s);
                     unpack<DT, kVec>(f[k], s);                       // the norm is that of the stored row
                 }
             }
         }
-        float sum[1] = {0.0f};
+        if constexpr (!kVec) fetch.start(row + step, 0);
+        V part = all<V>(0.0f);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
 #pragma unroll
-            for (int e = 0; e < E; ++e) sum[0] += f[k][e];
-        group_sum<1>(sum, warps, red[turn]);
+            for (int e = 0; e < P; ++e) part = part + f[k][e];
+        float sum[1] = {total(part)};
+        group_sum<1>(sum, warps, g, red[turn]);
         turn ^= 1u;
-        const float mean = sum[0] / a.count;
-        float sq[1] = {0.0f};
+        const float mean = quotient(sum[0], a.count, a.inverse);
+        part = all<V>(0.0f);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
             if (lane + k * a.group < a.packs)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float d = f[k][e] - mean;
-                    sq[0] = fmaf(d, d, sq[0]);
+                for (int e = 0; e < P; ++e) {
+                    f[k][e] = f[k][e] + all<V>(-mean);
+                    part = mad(f[k][e], f[k][e], part);
                 }
-        group_sum<1>(sq, warps, red[turn]);
+        float sq[1] = {total(part)};
+        group_sum<1>(sq, warps, g, red[turn]);
         turn ^= 1u;
-        const float rstd = 1.0f / sqrtf(sq[0] / a.count + a.eps);
+        const float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps));
         if (live && lane == 0u) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
+        void* to = row_at(a.y, (size_t)row, a.y_stride);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
             const unsigned i = lane + k * a.group;
             if (live && i < a.packs) {
-                float w[E], b[E];
+                V wf[P], bf[P];
+                w.get(wf, k);
+                b.get(bf, k);
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = 1.0f, b[e] = 0.0f;
-                if (a.weight) load_params<PT, E>(w, a.weight, i);
-                if (a.bias) load_params<PT, E>(b, a.bias, i);
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[k][e] = fmaf((f[k][e] - mean) * rstd, w[e], b[e]);
-                store_pack<DT, kVec>(row_at(a.y, row, a.y_stride), i, pack<DT, kVec>(f[k]));
+                for (int e = 0; e < P; ++e) f[k][e] = mad(f[k][e] * all<V>(rstd), wf[e], bf[e]);
+                store_pack<DT, kVec>(to, i, pack<DT, kVec>(f[k]));
             }
         }
+        stage = stage + 1u == kDepth ? 0u : stage + 1u;
     }
     pdl_trigger();
 }
 
 // Rows longer than a block's registers hold: one block per row, which reads the row again for each of the three steps.
-template <int DT, int PT>
+template <int DT, int PT, bool kVec>
 __global__ void __launch_bounds__(1024) k_norm_forward_long(const NormArgs a)
 {
+    constexpr int E = Pack<DT, kVec>::kElems;
     __shared__ float red[2][32];
     pdl_wait();
     const unsigned warps = blockDim.x / 32u;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const void* x = row_at(a.x, row, a.x_stride);
         float sum[1] = {0.0f};
-        for (unsigned i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-            float f[1];
-            unpack<DT, false>(f, load_pack<DT, false>(x, i));
+#pragma unroll 4
+        for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) {
+            float f[E];
+            unpack<DT, kVec>(f, load_pack<DT, kVec>(x, i));
             if (a.residual) {
-                float r[1];
-                unpack<DT, false>(r, load_pack<DT, false>(row_at(a.residual, row, a.residual_stride), i));
-                f[0] = __fadd_rn(f[0], r[0]);
-                const Pack<DT, false> s = pack<DT, false>(f);
-                store_pack<DT, false>(row_at(a.summed, row, a.summed_stride), i, s);
-                unpack<DT, false>(f, s);
+                float r[E];
+                unpack<DT, kVec>(r, load_pack<DT, kVec>(row_at(a.residual, row, a.residual_stride), i));
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[e] = __fadd_rn(f[e], r[e]);
+                const Pack<DT, kVec> s = pack<DT, kVec>(f);
+                store_pack<DT, kVec>(row_at(a.summed, row, a.summed_stride), i, s);
+                unpack<DT, kVec>(f, s);
             }
-            sum[0] += f[0];
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[0] += f[e];
         }
         const void* s = a.residual ? row_at(a.summed, row, a.summed_stride) : x;         // this thread's own stores
-        group_sum<1>(sum, warps, red[0]);
-        const float mean = sum[0] / a.count;
+        group_sum<1>(sum, warps, 0u, red[0]);
+        const float mean = quotient(sum[0], a.count, a.inverse);
         float sq[1] = {0.0f};
-        for (unsigned i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-            float f[1];
-            unpack<DT, false>(f, load_pack<DT, false>(s, i));
-            sq[0] = fmaf(f[0] - mean, f[0] - mean, sq[0]);
+#pragma unroll 4
+        for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) {
+            float f[E];
+            unpack<DT, kVec>(f, load_pack<DT, kVec>(s, i));
+#pragma unroll
+            for (int e = 0; e < E; ++e) sq[0] = fmaf(f[e] - mean, f[e] - mean, sq[0]);
         }
-        group_sum<1>(sq, warps, red[1]);
-        const float rstd = 1.0f / sqrtf(sq[0] / a.count + a.eps);
+        group_sum<1>(sq, warps, 0u, red[1]);
+        const float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps));
         if (threadIdx.x == 0u) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        for (unsigned i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-            float f[1], w[1] = {1.0f}, b[1] = {0.0f};
-            unpack<DT, false>(f, load_pack<DT, false>(s, i));
-            if (a.weight) load_params<PT, 1>(w, a.weight, i);
-            if (a.bias) load_params<PT, 1>(b, a.bias, i);
-            f[0] = fmaf((f[0] - mean) * rstd, w[0], b[0]);
-            store_pack<DT, false>(row_at(a.y, row, a.y_stride), i, pack<DT, false>(f));
+#pragma unroll 4
+        for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) {
+            float f[E], w[E], b[E];
+            unpack<DT, kVec>(f, load_pack<DT, kVec>(s, i));
+            unpack_params<PT, E>(w, load_params<PT, E>(a.weight, i, kOne<PT>));
+            unpack_params<PT, E>(b, load_params<PT, E>(a.bias, i, 0u));
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[e], b[e]);
+            store_pack<DT, kVec>(row_at(a.y, row, a.y_stride), i, pack<DT, kVec>(f));
         }
     }
     pdl_trigger();
@@ -173,99 +289,136 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(const NormArgs a)
 // A block's groups take rows in turn and keep their columns' shares of dweight and dbias in registers from row to row;
 // at the end the block's groups are added and the block's share goes to the workspace, whose at most 148 rows
 // k_norm_params adds up.  Which rows a group takes depends on sizes and types alone, and so do the sums' orders.
+// Threads of a block, of which an SM has one, and rows fetched ahead (none: a row's single elements fill the registers).
+__host__ __device__ constexpr int norm_grad_threads(bool vec) { return vec ? 512 : 1024; }
+__host__ __device__ constexpr int norm_grad_depth(int packs, bool vec) { return !vec && packs > 4 ? 1 : packs == 1 ? 4 : 2; }
+
 template <int DT, int PT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(512, 1) k_norm_backward(const NormGradArgs a)
+__global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const NormGradArgs a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
+    constexpr int kDepth = norm_grad_depth(kPacks, kVec);
     __shared__ float red[2][64];
-    extern __shared__ float joined[];                                // [groups - 1][2][kPacks * group * E], if groups > 1
-    pdl_wait();
+    extern __shared__ uint4 ring[];                                  // in the end, the groups' shares: [groups - 1][2][kPacks * group * E]
     const unsigned warps = a.group / 32u, g = threadIdx.x / a.group, lane = threadIdx.x % a.group, groups = blockDim.x / a.group;
-    float dw[kPacks][E], db[kPacks][E];
+    const unsigned long long step = (unsigned long long)gridDim.x * groups;
+    unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
+    RowFetch<DT, kPacks, kVec, 3, kDepth> fetch = {{a.x, a.dy, a.dsummed}, {a.x_stride, a.dy_stride, a.dsummed_stride}, {true, true, a.dsummed != nullptr},
+                                                   a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
+    pdl_wait();
 #pragma unroll
-    for (int k = 0; k < kPacks; ++k)
+    for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
+    constexpr int P = kLanes<DT, kVec>;
+    using V = Lanes<kVec>;
+    V dw[kPacks][P], db[kPacks][P];
+    KeptParams<PT, E, kPacks, false> w;
 #pragma unroll
-        for (int e = 0; e < E; ++e) dw[k][e] = db[k][e] = 0.0f;
-    unsigned turn = 0;
-    for (unsigned long long base = (unsigned long long)blockIdx.x * groups; base < a.rows; base += (unsigned long long)gridDim.x * groups) {
-        const size_t row = base + g;
+    for (int k = 0; k < kPacks; ++k) {
+        const unsigned i = lane + k * a.group;
+        w.put(k, load_params<PT, E>(i < a.packs ? a.weight : nullptr, i, kOne<PT>));
+#pragma unroll
+        for (int e = 0; e < P; ++e) dw[k][e] = db[k][e] = all<V>(0.0f);
+    }
+    float next_mean = row < a.rows ? a.mean[row] : 0.0f, next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
+    unsigned turn = 0, stage = 0;
+    for (unsigned long long base = (unsigned long long)blockIdx.x * groups; base < a.rows; base += step, row += step) {
         const bool live = row < a.rows;
-        const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
-        Pack<DT, kVec> px[kPacks], pdy[kPacks];
-        float c[2] = {0.0f, 0.0f};
+        const float mean = next_mean, rstd = next_rstd;
+        if (row + step < a.rows) next_mean = a.mean[row + step], next_rstd = a.rstd[row + step];
+        constexpr bool kKeep = kPacks * E <= 16 && kDepth > 1;       // registers for a row's xh and g; otherwise they are formed again
+        V xh[kKeep ? kPacks : 1][P], gy[kKeep ? kPacks : 1][P], r[kDepth == 2 && !kVec ? kPacks : 1][P];
+        const auto normal = [&](V (&x)[P], V (&g)[P], V (&dy)[P], int k) {
+            V wf[P];
+            unpack<DT, kVec>(x, fetch.take(stage, 0, k));
+            unpack<DT, kVec>(dy, fetch.take(stage, 1, k));
+            w.get(wf, k);
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = lane + k * a.group;
-            if (live && i < a.packs) {
-                px[k] = load_pack<DT, kVec>(row_at(a.x, row, a.x_stride), i);
-                pdy[k] = load_pack<DT, kVec>(row_at(a.dy, row, a.dy_stride), i);
+            for (int e = 0; e < P; ++e) {
+                x[e] = (x[e] + all<V>(-mean)) * all<V>(rstd);
+                g[e] = dy[e] * wf[e];
             }
+        };
+        if constexpr (kVec) {
+            fetch.start(row + (kDepth - 1) * step, stage == 0u ? kDepth - 1 : stage - 1u);
+            copy_wait<kDepth - 1>();
+        } else if constexpr (kDepth == 1) {
+            fetch.start(row, 0);
         }
+        V c0s = all<V>(0.0f), c1s = all<V>(0.0f);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
             const unsigned i = lane + k * a.group;
             if (live && i < a.packs) {
-                float x[E], dy[E], w[E];
-                unpack<DT, kVec>(x, px[k]);
-                unpack<DT, kVec>(dy, pdy[k]);
+                V dy[P];
+                V (&x)[P] = xh[kKeep ? k : 0];
+                V (&g)[P] = gy[kKeep ? k : 0];
+                normal(x, g, dy, k);
+                if constexpr (!kVec && kDepth == 2)
+                    if (a.dsummed) unpack<DT, kVec>(r[k], fetch.take(stage, 2, k));
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = 1.0f;
-                if (a.weight) load_params<PT, E>(w, a.weight, i);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float xh = (x[e] - mean) * rstd, gy = dy[e] * w[e];
-                    c[0] += gy;
-                    c[1] = fmaf(gy, xh, c[1]);
-                    dw[k][e] = fmaf(dy[e], xh, dw[k][e]);
-                    db[k][e] += dy[e];
+                for (int e = 0; e < P; ++e) {
+                    c0s = c0s + g[e];
+                    c1s = mad(g[e], x[e], c1s);
+                    dw[k][e] = mad(dy[e], x[e], dw[k][e]);
+                    db[k][e] = db[k][e] + dy[e];
                 }
             }
         }
-        group_sum<2>(c, warps, red[turn]);
+        if constexpr (!kVec && kDepth == 2) fetch.start(row + step, 0);
+        float c[2] = {total(c0s), total(c1s)};
+        group_sum<2>(c, warps, g, red[turn]);
         turn ^= 1u;
-        const float c0 = c[0] / a.count, c1 = c[1] / a.count;
+        const V c0 = all<V>(-c[0] * a.inverse), c1 = all<V>(-c[1] * a.inverse);
+        void* to = row_at(a.dx, (size_t)row, a.dx_stride);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
             const unsigned i = lane + k * a.group;
             if (live && i < a.packs) {
-                float x[E], dy[E], w[E], r[E];
-                unpack<DT, kVec>(x, px[k]);
-                unpack<DT, kVec>(dy, pdy[k]);
-#pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = 1.0f, r[e] = 0.0f;
-                if (a.weight) load_params<PT, E>(w, a.weight, i);
-                if (a.dsummed) unpack<DT, kVec>(r, load_pack<DT, kVec>(row_at(a.dsummed, row, a.dsummed_stride), i));
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float xh = (x[e] - mean) * rstd;
-                    r[e] = fmaf(rstd, fmaf(dy[e], w[e], -c0) - xh * c1, r[e]);
+                V (&s)[P] = r[kDepth == 2 && !kVec ? k : 0];
+                V (&x)[P] = xh[kKeep ? k : 0];
+                V (&g)[P] = gy[kKeep ? k : 0];
+                if constexpr (!kKeep) {
+                    V dy[P];
+                    normal(x, g, dy, k);
                 }
-                store_pack<DT, kVec>(row_at(a.dx, row, a.dx_stride), i, pack<DT, kVec>(r));
+                if (!a.dsummed) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) s[e] = all<V>(0.0f);
+                } else if constexpr (kVec || kDepth == 1) {
+                    unpack<DT, kVec>(s, fetch.take(stage, 2, k));
+                }
+#pragma unroll
+                for (int e = 0; e < P; ++e) s[e] = mad(all<V>(rstd), mad(x[e], c1, g[e] + c0), s[e]);
+                store_pack<DT, kVec>(to, i, pack<DT, kVec>(s));
             }
         }
+        stage = stage + 1u == kDepth ? 0u : stage + 1u;
     }
     if (a.part) {
-        const unsigned half = kPacks * a.group * E;
+        float* joined = reinterpret_cast<float*>(ring);
+        if constexpr (kVec) copy_wait<0>();
+        __syncthreads();                                             // every thread is done with its slots
+        const unsigned columns = kPacks * a.group * E;
         if (g > 0u) {
-            float* to = joined + (size_t)(g - 1u) * 2u * half;
+            float* to = joined + (size_t)(g - 1u) * 2u * columns;
 #pragma unroll
             for (int k = 0; k < kPacks; ++k)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    to[(k * E + e) * a.group + lane] = dw[k][e];
-                    to[half + (k * E + e) * a.group + lane] = db[k][e];
+                    to[(k * E + e) * a.group + lane] = half(dw[k][e / 2], e);
+                    to[columns + (k * E + e) * a.group + lane] = half(db[k][e / 2], e);
                 }
         }
         __syncthreads();
         if (g == 0u) {
             for (unsigned o = 0; o + 1u < groups; ++o) {
-                const float* from = joined + (size_t)o * 2u * half;
+                const float* from = joined + (size_t)o * 2u * columns;
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k)
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        dw[k][e] += from[(k * E + e) * a.group + lane];
-                        db[k][e] += from[half + (k * E + e) * a.group + lane];
+                        half(dw[k][e / 2], e) += from[(k * E + e) * a.group + lane];
+                        half(db[k][e / 2], e) += from[columns + (k * E + e) * a.group + lane];
                     }
             }
             float* share = a.part + (size_t)blockIdx.x * 2u * a.part_stride;
@@ -275,10 +428,10 @@ __global__ void __launch_bounds__(512, 1) k_norm_backward(const NormGradArgs a)
                 if (i < a.packs) {
                     if constexpr (E % 4 == 0) {
 #pragma unroll
-                        for (int e = 0; e < E; e += 4) {
-                            *reinterpret_cast<float4*>(share + (size_t)i * E + e) = make_float4(dw[k][e], dw[k][e + 1], dw[k][e + 2], dw[k][e + 3]);
-                            *reinterpret_cast<float4*>(share + a.part_stride + (size_t)i * E + e) =
-                                make_float4(db[k][e], db[k][e + 1], db[k][e + 2], db[k][e + 3]);
+                        for (int e = 0; e < P; e += 2) {
+                            *reinterpret_cast<float4*>(share + (size_t)i * E + 2 * e) = make_float4(dw[k][e].x, dw[k][e].y, dw[k][e + 1].x, dw[k][e + 1].y);
+                            *reinterpret_cast<float4*>(share + a.part_stride + (size_t)i * E + 2 * e) =
+                                make_float4(db[k][e].x, db[k][e].y, db[k][e + 1].x, db[k][e + 1].y);
                         }
                     } else {
                         share[i] = dw[k][0];
@@ -292,9 +445,10 @@ __global__ void __launch_bounds__(512, 1) k_norm_backward(const NormGradArgs a)
 }
 
 // Rows longer than a block's registers hold; the block's shares are kept in the workspace from row to row.
-template <int DT, int PT>
+template <int DT, int PT, bool kVec>
 __global__ void __launch_bounds__(1024) k_norm_backward_long(const NormGradArgs a)
 {
+    constexpr int E = Pack<DT, kVec>::kElems;
     __shared__ float red[2][64];
     pdl_wait();
     const unsigned warps = blockDim.x / 32u;
@@ -305,61 +459,79 @@ __global__ void __launch_bounds__(1024) k_norm_backward_long(const NormGradArgs 
         const float mean = a.mean[row], rstd = a.rstd[row];
         const void *px = row_at(a.x, row, a.x_stride), *pdy = row_at(a.dy, row, a.dy_stride);
         float c[2] = {0.0f, 0.0f};
-        for (unsigned i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-            float x[1], dy[1], w[1] = {1.0f};
-            unpack<DT, false>(x, load_pack<DT, false>(px, i));
-            unpack<DT, false>(dy, load_pack<DT, false>(pdy, i));
-            if (a.weight) load_params<PT, 1>(w, a.weight, i);
-            const float xh = (x[0] - mean) * rstd, gy = dy[0] * w[0];
-            c[0] += gy;
-            c[1] = fmaf(gy, xh, c[1]);
-            if (share) {
-                share[i] = fmaf(dy[0], xh, first ? 0.0f : share[i]);
-                share[a.part_stride + i] = (first ? 0.0f : share[a.part_stride + i]) + dy[0];
+#pragma unroll 2
+        for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) {
+            float x[E], dy[E], w[E];
+            unpack<DT, kVec>(x, load_pack<DT, kVec>(px, i));
+            unpack<DT, kVec>(dy, load_pack<DT, kVec>(pdy, i));
+            unpack_params<PT, E>(w, load_params<PT, E>(a.weight, i, kOne<PT>));
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float xh = (x[e] - mean) * rstd, gy = dy[e] * w[e];
+                c[0] += gy;
+                c[1] = fmaf(gy, xh, c[1]);
+                if (share) {
+                    const size_t at = (size_t)i * E + e;
+                    share[at] = fmaf(dy[e], xh, first ? 0.0f : share[at]);
+                    share[a.part_stride + at] = (first ? 0.0f : share[a.part_stride + at]) + dy[e];
+                }
             }
         }
-        group_sum<2>(c, warps, red[turn]);
+        group_sum<2>(c, warps, 0u, red[turn]);
         turn ^= 1u;
-        const float c0 = c[0] / a.count, c1 = c[1] / a.count;
-        for (unsigned i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-            float x[1], dy[1], w[1] = {1.0f}, r[1] = {0.0f};
-            unpack<DT, false>(x, load_pack<DT, false>(px, i));
-            unpack<DT, false>(dy, load_pack<DT, false>(pdy, i));
-            if (a.weight) load_params<PT, 1>(w, a.weight, i);
-            if (a.dsummed) unpack<DT, false>(r, load_pack<DT, false>(row_at(a.dsummed, row, a.dsummed_stride), i));
-            r[0] = fmaf(rstd, fmaf(dy[0], w[0], -c0) - (x[0] - mean) * rstd * c1, r[0]);
-            store_pack<DT, false>(row_at(a.dx, row, a.dx_stride), i, pack<DT, false>(r));
+        const float c0 = c[0] * a.inverse, c1 = c[1] * a.inverse;
+#pragma unroll 2
+        for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) {
+            float x[E], dy[E], w[E], r[E];
+            unpack<DT, kVec>(x, load_pack<DT, kVec>(px, i));
+            unpack<DT, kVec>(dy, load_pack<DT, kVec>(pdy, i));
+            unpack_params<PT, E>(w, load_params<PT, E>(a.weight, i, kOne<PT>));
+#pragma unroll
+            for (int e = 0; e < E; ++e) r[e] = 0.0f;
+            if (a.dsummed) unpack<DT, kVec>(r, load_pack<DT, kVec>(row_at(a.dsummed, row, a.dsummed_stride), i));
+#pragma unroll
+            for (int e = 0; e < E; ++e) r[e] = fmaf(rstd, fmaf((mean - x[e]) * rstd, c1, fmaf(dy[e], w[e], -c0)), r[e]);
+            store_pack<DT, kVec>(row_at(a.dx, row, a.dx_stride), i, pack<DT, kVec>(r));
         }
     }
     pdl_trigger();
 }
 
-// Adds up the blocks' shares: 32 columns a block, whose 16 warps take the shares in turn and are then added in order.
+// Adds up the blocks' shares: a block has 32 columns, whose shares its 32 slices of 8 threads take in turn, four columns a
+// thread and all loads in flight, and adds the slices in order.
+constexpr int kSlices = 32;
 template <int PT>
-__global__ void __launch_bounds__(512) k_norm_params(const float* part, void* dweight, void* dbias, unsigned shares, unsigned hidden,
-                                                     unsigned part_stride, unsigned column_blocks, bool accumulate)
+__global__ void __launch_bounds__(8 * kSlices) k_norm_params(const float* part, void* dweight, void* dbias, unsigned shares, unsigned hidden,
+                                                             unsigned part_stride, unsigned column_blocks, bool accumulate)
 {
-    __shared__ float sum[16][33];
+    constexpr int kEach = (int)(kNormBlocks + kSlices - 1) / kSlices;
+    __shared__ float sum[kSlices][33];
     pdl_wait();
-    const unsigned which = blockIdx.x / column_blocks, column = blockIdx.x % column_blocks * 32u + (threadIdx.x & 31u), slice = threadIdx.x >> 5;
+    const unsigned which = blockIdx.x / column_blocks, column = blockIdx.x % column_blocks * 32u, slice = threadIdx.x / 8u, at = threadIdx.x % 8u * 4u;
     void* out = which ? dbias : dweight;
-    float acc = 0.0f;
-    if (out && column < hidden) {
-#pragma unroll 4
-        for (unsigned s = slice; s < shares; s += 16u) acc += part[((size_t)s * 2u + which) * part_stride + column];
-    }
-    sum[slice][threadIdx.x & 31u] = acc;
-    __syncthreads();
-    if (slice == 0u && out && column < hidden) {
+    if (out == nullptr) return;
+    float4 v[kEach];
 #pragma unroll
-        for (int s = 1; s < 16; ++s) acc += sum[s][threadIdx.x];
-        float f[1] = {acc};
+    for (int k = 0; k < kEach; ++k) {
+        const unsigned s = slice + k * kSlices;
+        v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (s < shares && column + at < part_stride) v[k] = *reinterpret_cast<const float4*>(part + ((size_t)s * 2u + which) * part_stride + column + at);
+    }
+#pragma unroll
+    for (int k = 1; k < kEach; ++k) v[0].x += v[k].x, v[0].y += v[k].y, v[0].z += v[k].z, v[0].w += v[k].w;
+    sum[slice][at] = v[0].x, sum[slice][at + 1u] = v[0].y, sum[slice][at + 2u] = v[0].z, sum[slice][at + 3u] = v[0].w;
+    __syncthreads();
+    const unsigned mine = column + threadIdx.x;
+    if (threadIdx.x < 32u && mine < hidden) {
+        float f[1] = {0.0f};
+#pragma unroll
+        for (int s = 0; s < kSlices; ++s) f[0] += sum[s][threadIdx.x];
         if (accumulate) {
             float old[1];
-            unpack<PT, false>(old, load_pack<PT, false>(out, column));
+            unpack<PT, false>(old, load_pack<PT, false>(out, mine));
             f[0] += old[0];
         }
-        store_pack<PT, false>(out, column, pack<PT, false>(f));
+        store_pack<PT, false>(out, mine, pack<PT, false>(f));
     }
     pdl_trigger();
 }
@@ -389,19 +561,36 @@ static int forward(const nuna_layernorm_t& n, unsigned flags, void* stream)
                          .rows(n.weight, n.hidden, 0, p).rows(n.bias, n.hidden, 0, p).ok;
     NormArgs a = {n.x, n.residual, n.weight, n.bias, n.summed, n.y, n.mean, n.rstd, bytes(n.x_stride), bytes(n.residual_stride),
                   bytes(n.summed_stride), bytes(n.y_stride), (unsigned)n.rows, (unsigned)n.hidden,
-                  (unsigned)(vec ? n.hidden * e / 16 : n.hidden), 0, n.eps, (float)n.hidden};
+                  (unsigned)(vec ? n.hidden * e / 16 : n.hidden), 0, n.eps, (float)n.hidden, 1.0f / (float)n.hidden};
     return with_param(n.dtype, n.param_dtype, [&](auto dt, auto pt) {
         constexpr int DT = decltype(dt)::value, PT = decltype(pt)::value;
-        const auto run = [&](auto kernel, int per_thread) {
-            a.group = group_for(a.packs, per_thread);
-            const unsigned groups = std::max(1u, 256u / a.group);
-            return launch_op(kernel, Shape{(a.rows + groups - 1) / groups, groups * a.group, 0, 1}, flags, stream, a);
+        // per_block: threads of a block (at least a group); per_sm: threads that an SM shall have
+        const auto run = [&](auto per_thread, auto is_vec, unsigned per_block, unsigned per_sm) {
+            constexpr int kPacks = decltype(per_thread)::value;
+            constexpr bool kVec = decltype(is_vec)::value;
+            a.group = group_for(a.packs, kPacks);
+            const unsigned groups = std::min(15u, std::max(1u, per_block / a.group)), threads = groups * a.group, blocks = (a.rows + groups - 1) / groups;
+            const unsigned smem = RowFetch<DT, kPacks, kVec, 2, norm_depth(kPacks, kVec)>::kSlots * 16u * threads;
+            const int ok = smem > 32 * 1024 ? allow_smem<k_norm_forward<DT, PT, kPacks, kVec>>(227 * 1024 - 1024) : NUNA_OK;
+            if (ok != NUNA_OK) return ok;
+            const unsigned resident = std::max(1u, std::min(per_sm / threads, 227u * 1024u / (smem + 2048u)));
+            return launch_op(k_norm_forward<DT, PT, kPacks, kVec>, Shape{std::min(blocks, kSms * resident), threads, smem, 1}, flags, stream, a);
         };
-        if (vec && a.packs <= 128) return run(k_norm_forward<DT, PT, 1, true>, 1);
-        if (vec && a.packs <= 4096) return run(k_norm_forward<DT, PT, 4, true>, 4);
-        if (!vec && a.packs <= 1024) return run(k_norm_forward<DT, PT, 4, false>, 4);
-        if (!vec && a.packs <= 16384) return run(k_norm_forward<DT, PT, 16, false>, 16);
-        return launch_op(k_norm_forward_long<DT, PT>, Shape{std::min(a.rows, kSms * 2u), 1024, 0, 1}, flags, stream, a);
+        using Yes = std::true_type;
+        using No = std::false_type;
+        // Few rows: as many threads as a row has vectors, for its latency (1 x 8192 bf16 3.3 us, 4.8 with four vectors a thread).
+        // Many: four vectors a thread, so that a warp's part in the sums (40 instructions) is small beside its elements, and two
+        // blocks, each of which works while the other one sums (4096 x 8192 bf16 without residual 25.0 us; two vectors a
+        // thread in one block 37).  With a residual it is the four streams' traffic that bounds long rows, and fewer rows at a
+        // time are ahead: one block with two vectors a thread, where its groups fill it (4096 x 8192 44.4 against 47.1 us, 8192
+        // x 4096 44.1 | 46.8; but 32768 x 1024 55 | 46.4).
+        if (vec && (a.packs <= 32 || (a.packs <= 1024 && a.rows <= 2 * kSms))) return run(Num<1>{}, Yes{}, 256, 1024);
+        if (vec && a.residual && a.packs >= 480 && a.packs <= 1024 && 512u % group_for(a.packs, 2) == 0u) return run(Num<2>{}, Yes{}, 512, 512);
+        if (vec && a.packs <= 64) return run(Num<2>{}, Yes{}, 256, 512);
+        if (vec && a.packs <= 2048) return run(Num<4>{}, Yes{}, 256, 512);
+        if (!vec && a.packs <= 1024) return run(Num<4>{}, No{}, 256, 1024);
+        if (!vec && a.packs <= 8192) return run(Num<8>{}, No{}, 256, 1024);
+        return launch_op(vec ? k_norm_forward_long<DT, PT, true> : k_norm_forward_long<DT, PT, false>, Shape{std::min(a.rows, kSms * 2u), 1024, 0, 1}, flags, stream, a);
     });
 }
 
@@ -416,7 +605,7 @@ static int backward(const nuna_layernorm_grad_t& n, unsigned flags, void* stream
     unsigned shares = 0;
     NormGradArgs a = {n.dy, n.x, n.weight, n.dsummed, n.mean, n.rstd, n.dx, params ? static_cast<float*>(n.workspace) : nullptr,
                       bytes(n.dy_stride), bytes(n.x_stride), bytes(n.dsummed_stride), bytes(n.dx_stride), (unsigned)n.rows, (unsigned)n.hidden,
-                      (unsigned)(vec ? n.hidden * e / 16 : n.hidden), 0, (unsigned)((n.hidden + 3) / 4 * 4), (float)n.hidden};
+                      (unsigned)(vec ? n.hidden * e / 16 : n.hidden), 0, (unsigned)((n.hidden + 3) / 4 * 4), (float)n.hidden, 1.0f / (float)n.hidden};
     int st = n.rows == 0 ? NUNA_OK : with_param(n.dtype, n.param_dtype, [&](auto dt, auto pt) {
         constexpr int DT = decltype(dt)::value, PT = decltype(pt)::value;
         const auto run = [&](auto per_thread, auto is_vec) {
@@ -424,9 +613,10 @@ static int backward(const nuna_layernorm_grad_t& n, unsigned flags, void* stream
             constexpr bool kVec = decltype(is_vec)::value;
             constexpr int E = Pack<DT, kVec>::kElems;
             a.group = group_for(a.packs, kPacks);
-            const unsigned groups = std::max(1u, 512u / a.group);
+            const unsigned groups = std::min(15u, std::max(1u, (unsigned)norm_grad_threads(kVec) / a.group));
             shares = (unsigned)norm_blocks((a.rows + groups - 1) / groups);
-            const unsigned smem = params ? (groups - 1) * 2 * kPacks * a.group * E * 4 : 0;
+            const unsigned threads = groups * a.group, shares_smem = params ? (groups - 1) * 2 * kPacks * a.group * E * 4 : 0;
+            const unsigned smem = std::max(shares_smem, RowFetch<DT, kPacks, kVec, 3, norm_grad_depth(kPacks, kVec)>::kSlots * 16u * threads);
             if (smem > 32 * 1024) {
                 const int ok = allow_smem<k_norm_backward<DT, PT, kPacks, kVec>>(227 * 1024 - 1024);
                 if (ok != NUNA_OK) return ok;
@@ -435,18 +625,19 @@ static int backward(const nuna_layernorm_grad_t& n, unsigned flags, void* stream
         };
         using Yes = std::true_type;
         using No = std::false_type;
-        if (vec && a.packs <= 512) return run(Num<1>{}, Yes{});
+        // Two vectors a thread: with four, xh and g have to be formed twice (4096 x 8192 bf16 73 us against 49.7).
+        if (vec && a.packs <= 32) return run(Num<1>{}, Yes{});
         if (vec && a.packs <= 1024) return run(Num<2>{}, Yes{});
         if (vec && a.packs <= 2048) return run(Num<4>{}, Yes{});
-        if (!vec && a.packs <= 1024) return run(Num<2>{}, No{});
-        if (!vec && a.packs <= 8192) return run(Num<16>{}, No{});
+        if (!vec && a.packs <= 4096) return run(Num<4>{}, No{});
+        if (!vec && a.packs <= 8192) return run(Num<8>{}, No{});
         shares = (unsigned)norm_blocks(a.rows);
-        return launch_op(k_norm_backward_long<DT, PT>, Shape{shares, 1024, 0, 1}, flags, stream, a);
+        return launch_op(vec ? k_norm_backward_long<DT, PT, true> : k_norm_backward_long<DT, PT, false>, Shape{shares, 1024, 0, 1}, flags, stream, a);
     });
     if (st != NUNA_OK || !params || (accumulate && n.rows == 0)) return st;
     const unsigned column_blocks = (a.hidden + 31u) / 32u;
     return with_dtype(n.param_dtype, [&](auto pt) {
-        return launch_op(k_norm_params<decltype(pt)::value>, Shape{2 * column_blocks, 512, 0, 1}, flags, stream, a.part, n.dweight, n.dbias, shares,
+        return launch_op(k_norm_params<decltype(pt)::value>, Shape{2 * column_blocks, 8 * kSlices, 0, 1}, flags, stream, a.part, n.dweight, n.dbias, shares,
                          a.hidden, a.part_stride, column_blocks, accumulate);
     });
 }

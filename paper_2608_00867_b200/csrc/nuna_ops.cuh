@@ -6,6 +6,7 @@
 
 #include <cstdio>
 #include <cstring>
+#include <type_traits>
 
 #include "nuna_device.cuh"
 #include "nuna_internal.h"
@@ -182,26 +183,59 @@ __device__ __forceinline__ Pack<DT, kVec> pack(const float (&f)[Pack<DT, kVec>::
     return p;
 }
 
-// N consecutive parameters of type PT from element i * N on, in binary32 (N of 1, 4 or 8; vectors if more than one).
+// N consecutive parameters of type PT (1, 4 or 8; vectors if more than one), kept as they are stored.
+template <int PT, int N> struct Params {
+    static constexpr int kWords = PT == kF32 ? N : (N + 1) / 2;
+    uint32_t w[kWords];
+};
+
+// Those from element i * N on; `fill` (a pattern of PT's type) where there are no parameters.
 template <int PT, int N>
-__device__ __forceinline__ void load_params(float (&f)[N], const void* base, size_t i)
+__device__ __forceinline__ Params<PT, N> load_params(const void* base, size_t i, uint32_t fill)
 {
-    if constexpr (N == 1) {
-        unpack<PT, false>(f, load_pack<PT, false>(base, i));
-    } else if constexpr (PT == kF32) {
+    Params<PT, N> p;
+    if (base == nullptr) {
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) {
-            const uint4 v = *(static_cast<const uint4*>(base) + i * (N / 4) + k);
-            f[4 * k] = __uint_as_float(v.x), f[4 * k + 1] = __uint_as_float(v.y);
-            f[4 * k + 2] = __uint_as_float(v.z), f[4 * k + 3] = __uint_as_float(v.w);
-        }
+        for (int k = 0; k < Params<PT, N>::kWords; ++k) p.w[k] = fill;
+    } else if constexpr (N == 1) {
+        p.w[0] = load_pack<PT, false>(base, i).w[0];
     } else {
-        static_assert(N == 8, "a vector of 16-bit parameters");
-        const uint4 v = *(static_cast<const uint4*>(base) + i);
-        widen_word<PT>(f[0], f[1], v.x), widen_word<PT>(f[2], f[3], v.y);
-        widen_word<PT>(f[4], f[5], v.z), widen_word<PT>(f[6], f[7], v.w);
+#pragma unroll
+        for (int k = 0; k < Params<PT, N>::kWords; k += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const uint32_t*>(base) + i * Params<PT, N>::kWords + k);
+            p.w[k] = v.x, p.w[k + 1] = v.y, p.w[k + 2] = v.z, p.w[k + 3] = v.w;
+        }
+    }
+    return p;
+}
+
+// One, as load_params' fill: both halves of a word for the 16-bit types.
+template <int PT> constexpr uint32_t kOne = PT == kF32 ? 0x3F800000u : PT == kBf16 ? 0x3F803F80u : 0x3C003C00u;
+
+template <int PT, int N>
+__device__ __forceinline__ void unpack_params(float (&f)[N], const Params<PT, N>& p)
+{
+    if constexpr (PT == kF32) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = __uint_as_float(p.w[k]);
+    } else if constexpr (N == 1) {
+        float unused;
+        widen_word<PT>(f[0], unused, p.w[0]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) widen_word<PT>(f[2 * k], f[2 * k + 1], p.w[k]);
     }
 }
+
+// Copies 16 bytes to shared memory without a register; the thread waits for its own copies, group by group.
+__device__ __forceinline__ void copy_async(uint32_t to_shared, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to_shared), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most kLeft of the thread's latest groups are still on their way.
+template <int kLeft>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(kLeft) : "memory"); }
 
 template <typename T>
 __device__ __forceinline__ T* row_at(T* base, size_t row, size_t stride_bytes)
@@ -215,6 +249,80 @@ __device__ __forceinline__ const void* row_at(const void* base, size_t row, size
 __device__ __forceinline__ void* row_at(void* base, size_t row, size_t stride_bytes)
 {
     return reinterpret_cast<void*>(reinterpret_cast<uintptr_t>(base) + row * stride_bytes);
+}
+
+// Pairs of binary32 in one instruction (sm_100's f32x2 forms: each half rounds as the plain instruction does).  The
+// element-wise loops of the norm are bound by instruction issue as much as by memory, and these halve their arithmetic.
+struct Two {
+    float x, y;
+};
+__device__ __forceinline__ Two operator+(Two a, Two b)
+{
+    Two d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b)
+{
+    Two d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two mad(Two a, Two b, Two c)
+{
+    Two d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float mad(float a, float b, float c) { return fmaf(a, b, c); }
+
+// What a pack's arithmetic is done in: pairs, or for a single element a float.
+template <bool kVec> using Lanes = std::conditional_t<kVec, Two, float>;
+template <typename V> __device__ __forceinline__ V all(float v);
+template <> __device__ __forceinline__ Two all<Two>(float v) { return {v, v}; }
+template <> __device__ __forceinline__ float all<float>(float v) { return v; }
+__device__ __forceinline__ float total(Two v) { return v.x + v.y; }
+__device__ __forceinline__ float total(float v) { return v; }
+__device__ __forceinline__ float& half(Two& v, int i) { return i % 2 ? v.y : v.x; }
+__device__ __forceinline__ float& half(float& v, int) { return v; }
+
+template <int DT, bool kVec> constexpr int kLanes = (Pack<DT, kVec>::kElems + 1) / 2;
+
+template <int DT, bool kVec>
+__device__ __forceinline__ void unpack(Two (&f)[kLanes<DT, kVec>], const Pack<DT, kVec>& p)
+{
+    float v[Pack<DT, kVec>::kElems];
+    unpack<DT, kVec>(v, p);
+#pragma unroll
+    for (int i = 0; i < kLanes<DT, kVec>; ++i) f[i] = {v[2 * i], v[2 * i + 1]};
+}
+template <int DT, bool kVec>
+__device__ __forceinline__ Pack<DT, kVec> pack(const Two (&f)[kLanes<DT, kVec>])
+{
+    float v[Pack<DT, kVec>::kElems];
+#pragma unroll
+    for (int i = 0; i < kLanes<DT, kVec>; ++i) v[2 * i] = f[i].x, v[2 * i + 1] = f[i].y;
+    return pack<DT, kVec>(v);
+}
+// f += the pack's elements: one instruction for a 16-bit element, none for widening it.
+template <int DT, bool kVec>
+__device__ __forceinline__ void add_pack(Lanes<kVec> (&f)[kLanes<DT, kVec>], const Pack<DT, kVec>& p)
+{
+    if constexpr (DT == kF32) {
+        Lanes<kVec> r[kLanes<DT, kVec>];
+        unpack<DT, kVec>(r, p);
+#pragma unroll
+        for (int i = 0; i < kLanes<DT, kVec>; ++i) f[i] = f[i] + r[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLanes<DT, kVec>; ++i) {
+            half(f[i], 0) = add_narrow<DT>(half(f[i], 0), (uint16_t)p.w[i]);
+            if (kVec) half(f[i], 1) = add_narrow<DT>(half(f[i], 1), (uint16_t)(p.w[i] >> 16));
+        }
+    }
 }
 
 template <int N>

@@ -16,54 +16,57 @@ struct LookupArgs {
     void* out;
     size_t table_stride, out_stride;                                 // bytes
     long long vocab_start;
-    unsigned long long units;                                        // tokens * chunks
+    unsigned tokens, units;                                          // units: (tokens / kTokens) * chunks
     unsigned vocab_rows, packs, chunks, group;                       // packs in a row, chunks of a row, threads of a chunk
     float scale;
-    bool wide;                                                       // ids are int64
 };
 
-// The row of the slice that id i names, or -1.
-__device__ __forceinline__ long long slice_row(const void* ids, bool wide, size_t i, long long start, unsigned rows)
-{
-    const long long id = wide ? static_cast<const volatile long long*>(ids)[i] : (long long)static_cast<const volatile int*>(ids)[i];
-    // without overflow: id - start is formed only where it is small
-    if (id < start || (unsigned long long)id - (unsigned long long)start >= rows) return -1;
-    return id - start;
-}
-
-// One chunk of one token's row per group of threads, kPacks packs a thread, all of them in flight at once.
-template <int DT, int kPacks, bool kVec>
+// One chunk of kTokens tokens' rows per group of threads, kPacks packs a thread and token: the tokens' ids are fetched together,
+// and then all of their packs.
+template <typename Id, int DT, int kTokens, int kPacks, bool kVec>
 __global__ void __launch_bounds__(256) k_embedding_lookup(const LookupArgs a)
 {
-    constexpr int E = Pack<DT, kVec>::kElems;
+    using V = Lanes<kVec>;
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
+    const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
     if (unit < a.units) {
-        const size_t token = unit / a.chunks;
-        const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
-        const long long row = slice_row(a.ids, a.wide, token, a.vocab_start, a.vocab_rows);
-        Pack<DT, kVec> p[kPacks];
+        const unsigned first = unit / a.chunks * kTokens, from = unit % a.chunks * a.group * kPacks + lane;
+        long long id[kTokens];
+        Pack<DT, kVec> p[kTokens][kPacks];
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = from + k * a.group;
+        for (int t = 0; t < kTokens; ++t) id[t] = first + t < a.tokens ? load_id(static_cast<const Id*>(a.ids) + first + t) : -1;
+        unsigned found = 0;
 #pragma unroll
-            for (int w = 0; w < Pack<DT, kVec>::kWords; ++w) p[k].w[w] = 0u;
-            if (row >= 0 && i < a.packs) p[k] = load_pack<DT, kVec>(row_at(a.table, (size_t)row, a.table_stride), i);
-        }
+        for (int t = 0; t < kTokens; ++t) {
+            const unsigned long long row = (unsigned long long)id[t] - (unsigned long long)a.vocab_start;
+            const bool mine = id[t] >= a.vocab_start && row < a.vocab_rows;
+            const void* at = row_at(a.table, (size_t)row, a.table_stride);
+            if (mine) found |= 1u << t;
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = from + k * a.group;
-            if (i < a.packs) {
-                if (row >= 0) {
-                    float f[E];
-                    unpack<DT, kVec>(f, p[k]);
+            for (int k = 0; k < kPacks; ++k) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) f[e] *= a.scale;
-                    p[k] = pack<DT, kVec>(f);
-                }
-                store_pack<DT, kVec>(row_at(a.out, token, a.out_stride), i, p[k]);
+                for (int w = 0; w < Pack<DT, kVec>::kWords; ++w) p[t][k].w[w] = 0u;
+                if (mine && from + k * a.group < a.packs) p[t][k] = load_pack<DT, kVec>(at, from + k * a.group);
             }
+        }
+        if (a.scale == 1.0f) found = 0;                              // nothing to scale; the zeros of no row never are: the scale may be infinite
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) {
+            if (first + t >= a.tokens) break;
+            void* out = row_at(a.out, (size_t)first + t, a.out_stride);
+#pragma unroll
+            for (int k = 0; k < kPacks; ++k)
+                if (from + k * a.group < a.packs) {
+                    if (found >> t & 1u) {
+                        V f[kLanes<DT, kVec>];
+                        unpack<DT, kVec>(f, p[t][k]);
+#pragma unroll
+                        for (int e = 0; e < kLanes<DT, kVec>; ++e) f[e] = f[e] * all<V>(a.scale);
+                        p[t][k] = pack<DT, kVec>(f);
+                    }
+                    store_pack<DT, kVec>(out, from + k * a.group, p[t][k]);
+                }
         }
     }
     pdl_trigger();
@@ -73,120 +76,141 @@ __global__ void __launch_bounds__(256) k_embedding_lookup(const LookupArgs a)
 
 struct SortArgs {
     const void* ids;
-    unsigned *token[2], *id[2], *begin, *end, *count;
+    uint2* items[2];                                                 // token and row of the slice
+    unsigned *begin, *end, *count, *cut;
     long long vocab_start;
     unsigned tokens, vocab_rows, passes, bits;                       // bits of a digit
-    bool wide, clear;                                                // clear: rows without a token get end = 0
+    bool clear;                                                      // rows without a token get end = 0
 };
 
-// token[passes & 1 ^ 1] / id[...]: the tokens with a row in the slice, by row and then by token; begin / end: each row's run.
+// items[passes & 1 ^ 1]: the tokens with a row in the slice, by row and then by token; begin / end: each row's run; count: how
+// many tokens that is, and how many runs are cut; cut: where those begin, in no order (each of them is joined by itself).
+template <typename Id>
 __global__ void __launch_bounds__(1024) k_embedding_sort(const SortArgs a)
 {
     extern __shared__ unsigned smem[];
     pdl_wait();
     const unsigned bins = 1u << a.bits, threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
-    if (a.clear)
-        for (unsigned long long v = thread; v < a.vocab_rows; v += threads) a.end[v] = 0u;
-    unsigned n = a.tokens;
-    for (unsigned pass = 0; pass < a.passes; ++pass) {
-        const unsigned shift = pass * a.bits;
-        unsigned *token = a.token[pass & 1u], *id = a.id[pass & 1u];
-        const volatile unsigned *from_token = a.token[(pass & 1u) ^ 1u], *from_id = a.id[(pass & 1u) ^ 1u];
-        if (pass == 0u) {
-            n = sort_pass(n, bins, smem, nullptr,
-                [&](unsigned i) {
-                    const long long row = slice_row(a.ids, a.wide, i, a.vocab_start, a.vocab_rows);
-                    return row < 0 ? kNoDigit : (unsigned)row & (bins - 1u);
-                },
-                [&](unsigned i, unsigned d, unsigned first, unsigned rank) {
-                    if (d == kNoDigit) return;
-                    token[first + rank] = i;
-                    id[first + rank] = (unsigned)slice_row(a.ids, a.wide, i, a.vocab_start, a.vocab_rows);
-                });
-        } else {
-            sort_pass(n, bins, smem, nullptr,
-                [&](unsigned i) { return (from_id[i] >> shift) & (bins - 1u); },
-                [&](unsigned i, unsigned, unsigned first, unsigned rank) {
-                    token[first + rank] = from_token[i];
-                    id[first + rank] = from_id[i];
-                });
-        }
+    const Id* ids = static_cast<const Id*>(a.ids);
+    if (thread == 0u) a.count[1] = 0u;                               // like `end`, before the first pass
+    if (a.clear)                                                     // whose barriers order it
+        // 16 bytes a store; the rest of the last vector is the workspace's padding
+        for (unsigned long long v = thread; v * 4u < a.vocab_rows; v += threads) reinterpret_cast<uint4*>(a.end)[v] = make_uint4(0u, 0u, 0u, 0u);
+    const auto row_of = [&](long long id) {
+        const unsigned long long from = (unsigned long long)id - (unsigned long long)a.vocab_start;
+        return id >= a.vocab_start && from < a.vocab_rows ? (unsigned)from : kNoDigit;
+    };
+    uint2 *to = a.items[0], *from = a.items[1];
+    const unsigned n = sort_pass<long long>(a.tokens, bins, smem, nullptr,
+        [&](unsigned i) { return load_id(ids + i); },
+        [&](long long id) {
+            const unsigned row = row_of(id);
+            return row == kNoDigit ? kNoDigit : row & (bins - 1u);
+        },
+        [&](unsigned i, long long id, unsigned d, unsigned first, unsigned rank) {
+            if (d != kNoDigit) to[first + rank] = make_uint2(i, row_of(id));
+        });
+    for (unsigned pass = 1; pass < a.passes; ++pass) {
+        uint2* last = to;
+        to = from, from = last;
+        sort_pass<uint2>(n, bins, smem, nullptr, [&](unsigned i) { return load_shared_by_cluster(from + i); },
+            [&](uint2 item) { return (item.y >> (pass * a.bits)) & (bins - 1u); },
+            [&](unsigned, uint2 item, unsigned, unsigned first, unsigned rank) { to[first + rank] = item; });
     }
-    const volatile unsigned* id = a.id[(a.passes & 1u) ^ 1u];
     for (unsigned long long p = thread; p < n; p += threads) {
-        const unsigned v = id[p];
-        if (p == 0 || id[p - 1] != v) a.begin[v] = (unsigned)p;
-        if (p + 1 == n || id[p + 1] != v) a.end[v] = (unsigned)p + 1u;
+        const unsigned v = load_shared_by_cluster(to + p).y;
+        const unsigned left = p > 0 ? load_shared_by_cluster(to + p - 1).y : kNoDigit, right = p + 1 < n ? load_shared_by_cluster(to + p + 1).y : kNoDigit;
+        if (left != v) a.begin[v] = (unsigned)p;
+        if (right != v) a.end[v] = (unsigned)p + 1u;
+        if (left != v && p + kRunPart < n && load_shared_by_cluster(to + p + kRunPart).y == v) a.cut[atomicAdd(a.count + 1, 1u)] = (unsigned)p;
     }
-    if (thread == 0u) *a.count = n;
+    if (thread == 0u) a.count[0] = n;
     pdl_trigger();
 }
 
 struct TableArgs {
     const void* dout;
     void* dtable;
-    const unsigned *token, *id, *begin, *end, *count;
+    const uint2* items;                                              // (token, row) by row
+    const unsigned *begin, *end, *count, *cut;
     float* part;                                                     // [parts][2][part_stride]
     size_t dout_stride, dtable_stride;                               // bytes
-    unsigned long long row_units;                                    // table rows (positions, if accumulating) * chunks
+    unsigned rows, row_units, each;                                  // table rows (positions, if accumulating); (rows / each) * chunks
     unsigned parts, part_blocks;                                     // cuts of the positions, blocks that add them
-    unsigned hidden, packs, chunks, group, part_stride;
+    unsigned packs, chunks, group, part_stride;
+    unsigned hidden;
     float scale;
-    bool accumulate;
+    bool accumulate, whole_sectors;                                  // rows of dtable are at 32-byte addresses
 };
 
-// acc += the packs i + k * group of the rows of dout that positions p ... end-1 name, in their order.
+// acc += the packs from + k * group of the rows of dout that positions p ... end-1 name, in their order.  A warp fetches 32
+// positions' tokens at once, and then kAhead rows.  All lanes of a warp have the same run.
 template <int DT, int kPacks, bool kVec>
 __device__ __forceinline__ void add_run(float (&acc)[kPacks][Pack<DT, kVec>::kElems], const TableArgs& a, unsigned p, unsigned end, unsigned from)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
-    constexpr int kAhead = kPacks >= 4 ? 2 : 4;                      // rows in flight
-    for (; p < end; p += kAhead) {
-        Pack<DT, kVec> v[kAhead][kPacks];
+    constexpr int kAhead = kVec ? 4 : 8;
+    for (; p < end; p += 32u) {
+        const unsigned lane = threadIdx.x & 31u, n = end - p < 32u ? end - p : 32u;
+        const unsigned token = lane < n ? a.items[p + lane].x : 0u;
+        for (unsigned r0 = 0; r0 < n; r0 += kAhead) {
+            Pack<DT, kVec> v[kAhead][kPacks];
 #pragma unroll
-        for (int r = 0; r < kAhead; ++r)
-            if (p + r < end) {
-                const void* row = row_at(a.dout, a.token[p + r], a.dout_stride);
+            for (int r = 0; r < kAhead; ++r) {
+                const void* row = row_at(a.dout, __shfl_sync(0xFFFFFFFFu, token, r0 + r), a.dout_stride);
+                if (r0 + r < n)
 #pragma unroll
-                for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs) v[r][k] = load_pack<DT, kVec>(row, from + k * a.group);
+                    for (int k = 0; k < kPacks; ++k)
+                        if (from + k * a.group < a.packs) v[r][k] = load_pack<DT, kVec>(row, from + k * a.group);
             }
 #pragma unroll
-        for (int r = 0; r < kAhead; ++r)
-            if (p + r < end)
+            for (int r = 0; r < kAhead; ++r)
+                if (r0 + r < n)
 #pragma unroll
-                for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs) {
-                        float f[E];
-                        unpack<DT, kVec>(f, v[r][k]);
+                    for (int k = 0; k < kPacks; ++k)
+                        if (from + k * a.group < a.packs) {
+                            float f[E];
+                            unpack<DT, kVec>(f, v[r][k]);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) acc[k][e] += f[e];
-                    }
+                            for (int e = 0; e < E; ++e) acc[k][e] += f[e];
+                        }
+        }
     }
 }
 
 // E values of dtable's type GT from element i * E of a row on: rne(scale * sum), or added to what is there.
 template <int GT, int E>
-__device__ __forceinline__ void put_gradient(void* row, unsigned i, const float (&sum)[E], float scale, bool accumulate)
+__device__ __forceinline__ void put_gradient(const TableArgs& a, void* row, unsigned i, float (&sum)[E])
 {
     constexpr bool kVec = E > 1;
     constexpr int G = Pack<GT, kVec>::kElems, kParts = E / G;
 #pragma unroll
     for (int q = 0; q < kParts; ++q) {
+        float old[G];
+        if (a.accumulate) unpack<GT, kVec>(old, load_pack<GT, kVec>(row, (size_t)i * kParts + q));
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+            sum[q * G + e] *= a.scale;
+            if (a.accumulate) sum[q * G + e] = __fadd_rn(old[e], sum[q * G + e]);
+        }
+    }
+    if constexpr (GT == kF32 && E == 8) {
+        if (a.whole_sectors) {
+            store8(static_cast<float*>(row) + (size_t)i * 8u, sum);
+            return;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
         float f[G];
 #pragma unroll
-        for (int e = 0; e < G; ++e) f[e] = sum[q * G + e] * scale;
-        if (accumulate) {
-            float old[G];
-            unpack<GT, kVec>(old, load_pack<GT, kVec>(row, (size_t)i * kParts + q));
-#pragma unroll
-            for (int e = 0; e < G; ++e) f[e] = __fadd_rn(old[e], f[e]);
-        }
+        for (int e = 0; e < G; ++e) f[e] = sum[q * G + e];
         store_pack<GT, kVec, true>(row, (size_t)i * kParts + q, pack<GT, kVec>(f));
     }
 }
 
-// Blocks below part_blocks add the parts of cut runs; the others take one chunk of a table row per group of threads.
+// Blocks below part_blocks add the parts of cut runs; the others take one chunk of `each` table rows per group of threads,
+// whose runs are fetched together: most rows of a large vocabulary have none, and are only written.
 template <int DT, int GT, int kPacks, bool kVec>
 __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
 {
@@ -194,94 +218,106 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     float acc[kPacks][E];
-#pragma unroll
-    for (int k = 0; k < kPacks; ++k)
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[k][e] = 0.0f;
     if (blockIdx.x < a.part_blocks) {
-        const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
-        const unsigned part = (unsigned)(unit / a.chunks / 2u), n = *a.count;
-        const bool last = unit / a.chunks % 2u != 0u;                // the run of the part's last position, or of its first
+        const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+        const unsigned part = unit / a.chunks, n = a.count[0], from = unit % a.chunks * a.group * kPacks + lane;
         const unsigned long long lo = (unsigned long long)part * kRunPart;
         if (part < a.parts && lo < n) {
             const unsigned hi = (unsigned)(lo + kRunPart < n ? lo + kRunPart : n);
-            const unsigned v = a.id[last ? hi - 1u : lo], b = a.begin[v], e = a.end[v];
-            if (e - b > kRunPart && !(last && b <= lo)) {
-                const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
+            const unsigned row[2] = {a.items[lo].y, a.items[hi - 1u].y};
+            for (int last = 0; last < 2; ++last) {                   // the run of the part's first position, and of its last if another
+                const unsigned v = row[last], b = a.begin[v], e = a.end[v];
+                if (e - b <= kRunPart || (last && b <= lo)) continue;
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k)
+#pragma unroll
+                    for (int x = 0; x < E; ++x) acc[k][x] = 0.0f;
                 add_run<DT, kPacks, kVec>(acc, a, b > lo ? b : (unsigned)lo, e < hi ? e : hi, from);
                 float* to = a.part + ((size_t)part * 2u + last) * a.part_stride;
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs)
-#pragma unroll
-                        for (int x = 0; x < E; ++x) to[(size_t)(from + k * a.group) * E + x] = acc[k][x];
+                    if (from + k * a.group < a.packs) {
+                        if constexpr (E == 8)      store8(to + (size_t)(from + k * a.group) * 8u, acc[k]);
+                        else if constexpr (E == 4) *reinterpret_cast<float4*>(to + (size_t)(from + k * a.group) * 4u) = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+                        else                       to[from + k * a.group] = acc[k][0];
+                    }
             }
         }
     } else {
-        const unsigned long long unit = (unsigned long long)(blockIdx.x - a.part_blocks) * groups + threadIdx.x / a.group;
+        const unsigned unit = (blockIdx.x - a.part_blocks) * groups + threadIdx.x / a.group;
         if (unit < a.row_units) {
-            unsigned v = (unsigned)(unit / a.chunks), b, e;
-            bool mine = true;
-            if (a.accumulate) {                                      // v is a position: the first of a run stands for its row
+            const unsigned first = unit / a.chunks * a.each, from = unit % a.chunks * a.group * kPacks + lane, me = threadIdx.x & 31u;
+            unsigned v = first + me, b = 0, e = 0;                   // of the row that this lane looks at
+            bool mine = me < a.each && v < a.rows;
+            if (mine && a.accumulate) {                              // a position: the first of a run stands for its row
                 const unsigned p = v;
-                mine = p < *a.count && (v = a.id[p], a.begin[v] == p);
-                b = p, e = mine ? a.end[v] : 0u;
-            } else {
-                e = a.end ? a.end[v] : 0u;                           // no tokens at all: nothing was sorted
-                b = e ? a.begin[v] : 0u;
+                mine = p < a.count[0];
+                if (mine) v = a.items[p].y, b = a.begin[v], e = a.end[v];
+                mine = mine && b == p;
+            } else if (mine && a.end) {                              // no tokens at all: nothing was sorted
+                e = a.end[v];
+                if (e) b = a.begin[v];
             }
-            if (mine && e - b <= kRunPart) {
-                const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
-                add_run<DT, kPacks, kVec>(acc, a, b, e, from);
-                void* row = row_at(a.dtable, v, a.dtable_stride);
+            const unsigned empty = __ballot_sync(0xFFFFFFFFu, mine && e == b), todo = __ballot_sync(0xFFFFFFFFu, mine && e != b && e - b <= kRunPart);
+            // Rows without a token: one after the other, they are only stores, of consecutive vectors by consecutive lanes.
+            constexpr int G = Pack<GT, kVec>::kElems, kParts = E / G;
+            Pack<GT, kVec> zero;
+#pragma unroll
+            for (int w = 0; w < Pack<GT, kVec>::kWords; ++w) zero.w[w] = 0u;
+            const unsigned zero_from = (from - lane) * kParts + lane;
+            for (unsigned left = empty; left; left &= left - 1u) {
+                void* row = row_at(a.dtable, (size_t)first + __ffs(left) - 1, a.dtable_stride);
+#pragma unroll
+                for (int k = 0; k < kPacks * kParts; ++k)
+                    if (zero_from + k * a.group < a.packs * kParts) store_pack<GT, kVec, true>(row, zero_from + k * a.group, zero);
+            }
+            for (unsigned left = todo; left; left &= left - 1u) {
+                const int r = __ffs(left) - 1;
+                const unsigned row_v = __shfl_sync(0xFFFFFFFFu, v, r), row_b = __shfl_sync(0xFFFFFFFFu, b, r), row_e = __shfl_sync(0xFFFFFFFFu, e, r);
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs) put_gradient<GT, E>(row, from + k * a.group, acc[k], a.scale, a.accumulate);
+#pragma unroll
+                    for (int x = 0; x < E; ++x) acc[k][x] = 0.0f;
+                add_run<DT, kPacks, kVec>(acc, a, row_b, row_e, from);
+                void* row = row_at(a.dtable, row_v, a.dtable_stride);
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k)
+                    if (from + k * a.group < a.packs) put_gradient<GT, E>(a, row, from + k * a.group, acc[k]);
             }
         }
     }
     pdl_trigger();
 }
 
-// Joins the parts of each cut run: the part in which it begins does it, one chunk per group of threads.
-template <int GT, int E, int kPacks>
+// Joins the parts of the cut runs, 128 columns of one run at a time: eight warps take its parts in turn, and are added in order.
+constexpr unsigned kJoinColumns = 128;
+template <int GT>
 __global__ void __launch_bounds__(256) k_embedding_join(const TableArgs a)
 {
+    __shared__ float4 sum[8][32];
     pdl_wait();
-    const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
-    const unsigned part = (unsigned)(unit / a.chunks), n = *a.count;
-    const unsigned long long lo = (unsigned long long)part * kRunPart;
-    if (part < a.parts && lo < n) {
-        const unsigned hi = (unsigned)(lo + kRunPart < n ? lo + kRunPart : n);
-        const unsigned v = a.id[hi - 1u], b = a.begin[v], e = a.end[v];
-        if (b >= lo && e - b > kRunPart) {
-            const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
-            const unsigned ends = (unsigned)((e - 1u) / kRunPart);
-#pragma unroll
-            for (int k = 0; k < kPacks; ++k) {
-                const unsigned i = from + k * a.group;
-                if (i < a.packs) {
-                    float acc[E];
-#pragma unroll
-                    for (int x = 0; x < E; ++x) acc[x] = 0.0f;
+    const unsigned slice = threadIdx.x >> 5, lane = threadIdx.x & 31u, chunks = (a.hidden + kJoinColumns - 1u) / kJoinColumns;
+    const unsigned long long todo = (unsigned long long)a.count[1] * chunks;
+    for (unsigned long long t = blockIdx.x; t < todo; t += gridDim.x) {
+        const unsigned b = a.cut[t / chunks], column = (unsigned)(t % chunks) * kJoinColumns, v = a.items[b].y, e = a.end[v];
+        const unsigned first = b / (unsigned)kRunPart, last = (e - 1u) / (unsigned)kRunPart;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (column + lane * 4u < a.part_stride) {
 #pragma unroll 4
-                    for (unsigned q = part; q <= ends; ++q) {
-                        const float* share = a.part + ((size_t)q * 2u + (q == part && b > lo)) * a.part_stride + (size_t)i * E;
-                        if constexpr (E % 4 == 0) {
-#pragma unroll
-                            for (int x = 0; x < E; x += 4) {
-                                const float4 s = *reinterpret_cast<const float4*>(share + x);
-                                acc[x] += s.x, acc[x + 1] += s.y, acc[x + 2] += s.z, acc[x + 3] += s.w;
-                            }
-                        } else {
-                            acc[0] += share[0];
-                        }
-                    }
-                    put_gradient<GT, E>(row_at(a.dtable, v, a.dtable_stride), i, acc, a.scale, a.accumulate);
-                }
+            for (unsigned q = first + slice; q <= last; q += 8u) {
+                const float4 f = *reinterpret_cast<const float4*>(a.part + ((size_t)q * 2u + (q == first && b % (unsigned)kRunPart != 0u)) * a.part_stride + column + lane * 4u);
+                s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
             }
         }
+        sum[slice][lane] = s;
+        __syncthreads();
+        if (threadIdx.x < kJoinColumns && column + threadIdx.x < a.hidden) {
+            float f[1] = {0.0f};
+#pragma unroll
+            for (int o = 0; o < 8; ++o) f[0] += reinterpret_cast<const float*>(sum[o])[threadIdx.x];
+            put_gradient<GT, 1>(a, row_at(a.dtable, v, a.dtable_stride), column + threadIdx.x, f);
+        }
+        __syncthreads();
     }
     pdl_trigger();
 }
@@ -292,12 +328,14 @@ struct RowShape {
     unsigned group, chunks;
 };
 
-// Threads and chunks for a row of `packs` packs, kPacks a thread: chunks of at most 256 threads.
-static RowShape row_shape(size_t packs, int per_thread)
+// Threads (at most `most`) and chunks, of about the same length, for a row of `packs` packs, kPacks a thread.
+static RowShape row_shape(size_t packs, int per_thread, size_t most = 256)
 {
-    const size_t threads = (packs + per_thread - 1) / per_thread, group = std::min<size_t>(256, (threads + 31) / 32 * 32);
-    return {(unsigned)group, (unsigned)((threads + group - 1) / group)};
+    const size_t threads = (packs + per_thread - 1) / per_thread, chunks = (threads + most - 1) / most;
+    return {(unsigned)(((threads + chunks - 1) / chunks + 31) / 32 * 32), (unsigned)chunks};
 }
+
+constexpr unsigned long long kMaxUnits = 0xFFFFFF00ull;              // 32 bits count the units of a launch
 
 static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
 {
@@ -307,24 +345,26 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
     a.ids = n.ids, a.table = n.table, a.out = n.out;
     a.table_stride = (n.table_stride ? n.table_stride : n.hidden) * e;
     a.out_stride = (n.out_stride ? n.out_stride : n.hidden) * e;
-    a.vocab_start = n.vocab_start, a.vocab_rows = (unsigned)n.vocab_rows;
+    a.vocab_start = n.vocab_start, a.vocab_rows = (unsigned)n.vocab_rows, a.tokens = (unsigned)n.tokens;
     a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
-    a.scale = n.scale, a.wide = n.id_bytes == 8;
-    return with_dtype(n.dtype, [&](auto dt) {
+    a.scale = n.scale;
+    const auto typed = [&](auto id, auto dt) {
+        using Id = decltype(id);
         constexpr int DT = decltype(dt)::value;
-        const auto run = [&](auto kernel, int per_thread) {
+        const auto run = [&](auto kernel, int tokens, int per_thread) {
             const RowShape s = row_shape(a.packs, per_thread);
             a.group = s.group, a.chunks = s.chunks;
-            a.units = (unsigned long long)n.tokens * s.chunks;
+            const unsigned long long units = (n.tokens + tokens - 1) / tokens * s.chunks;
+            if (units > kMaxUnits) return (int)NUNA_ERR_TOO_LARGE;
+            a.units = (unsigned)units;
             const unsigned groups = 256u / s.group;
-            const unsigned long long grid = (a.units + groups - 1) / groups;
-            if (grid > kMaxExtent) return (int)NUNA_ERR_TOO_LARGE;
-            return launch_op(kernel, Shape{(unsigned)grid, groups * s.group, 0, 1}, flags, stream, a);
+            return launch_op(kernel, Shape{(unsigned)((units + groups - 1) / groups), groups * s.group, 0, 1}, flags, stream, a);
         };
-        const bool few = (unsigned long long)n.tokens * a.packs <= 4ull * kSms * 512ull;     // too few for every SM to hold four a thread
-        if (vec) return few ? run(k_embedding_lookup<DT, 1, true>, 1) : run(k_embedding_lookup<DT, 4, true>, 4);
-        return few ? run(k_embedding_lookup<DT, 1, false>, 1) : run(k_embedding_lookup<DT, 8, false>, 8);
-    });
+        const bool few = (unsigned long long)n.tokens * a.packs <= 4ull * kSms * 512ull;     // too few for every SM to hold more than one a thread
+        if (vec) return few ? run(k_embedding_lookup<Id, DT, 1, 1, true>, 1, 1) : run(k_embedding_lookup<Id, DT, 4, 2, true>, 4, 2);
+        return few ? run(k_embedding_lookup<Id, DT, 1, 1, false>, 1, 1) : run(k_embedding_lookup<Id, DT, 2, 8, false>, 2, 8);
+    };
+    return with_dtype(n.dtype, [&](auto dt) { return n.id_bytes == 8 ? typed((long long)0, dt) : typed(0, dt); });
 }
 
 static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* stream)
@@ -336,29 +376,33 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     const auto words = [&](size_t at) { return reinterpret_cast<unsigned*>(static_cast<char*>(n.workspace) + at); };
     SortArgs s = {};
     s.ids = n.ids, s.vocab_start = n.vocab_start, s.tokens = (unsigned)n.tokens, s.vocab_rows = (unsigned)n.vocab_rows;
-    s.wide = n.id_bytes == 8, s.clear = !accumulate;
-    for (int i = 0; i < 2; ++i) s.token[i] = words(w.token[i]), s.id[i] = words(w.id[i]);
-    s.begin = words(w.begin), s.end = words(w.end), s.count = words(w.count);
+    s.clear = !accumulate;
+    for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint2*>(words(w.items[i]));
+    s.begin = words(w.begin), s.end = words(w.end), s.count = words(w.count), s.cut = words(w.cut);
     unsigned bits = 1;
     while (bits < 32u && (n.vocab_rows - 1) >> bits) ++bits;
     s.passes = (bits + 9u) / 10u;                                    // digits of at most 10 bits: 1024 bins a warp fit a block's shared memory
     s.bits = (bits + s.passes - 1u) / s.passes;
     if (n.tokens) {
         const Shape sort = sort_shape(n.tokens, 1u << s.bits);
-        int st = sort.smem > 32 * 1024 ? allow_smem<k_embedding_sort>(sort_smem(kSortMaxWarps, 1024)) : NUNA_OK;
-        if (st != NUNA_OK || (st = launch_op(k_embedding_sort, sort, flags, stream, s)) != NUNA_OK) return st;
+        constexpr int kMost = sort_smem(kSortMaxWarps, 1024);
+        const bool wide = n.id_bytes == 8;
+        int st = sort.smem <= 32 * 1024 ? NUNA_OK : wide ? allow_smem<k_embedding_sort<long long>>(kMost) : allow_smem<k_embedding_sort<int>>(kMost);
+        if (st != NUNA_OK) return st;
+        if ((st = launch_op(wide ? k_embedding_sort<long long> : k_embedding_sort<int>, sort, flags, stream, s)) != NUNA_OK) return st;
     }
 
     const bool vec = VectorRows{true}.rows(n.dout, n.hidden, n.dout_stride, e).rows(n.dtable, n.hidden, n.dtable_stride, ge).ok;
     TableArgs a = {};
     a.dout = n.dout, a.dtable = n.dtable;
-    a.token = s.token[(s.passes & 1u) ^ 1u], a.id = s.id[(s.passes & 1u) ^ 1u], a.begin = s.begin, a.end = n.tokens ? s.end : nullptr, a.count = s.count;
+    a.items = s.items[(s.passes & 1u) ^ 1u], a.begin = s.begin, a.end = n.tokens ? s.end : nullptr, a.count = s.count, a.cut = s.cut;
     a.part = reinterpret_cast<float*>(words(w.part));
     a.dout_stride = (n.dout_stride ? n.dout_stride : n.hidden) * e;
     a.dtable_stride = (n.dtable_stride ? n.dtable_stride : n.hidden) * ge;
-    a.hidden = (unsigned)n.hidden, a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden), a.part_stride = (unsigned)((n.hidden + 3) / 4 * 4);
-    a.scale = n.scale, a.accumulate = accumulate;
+    a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden), a.part_stride = (unsigned)part_stride(n.hidden), a.hidden = (unsigned)n.hidden;
+    a.scale = n.scale, a.accumulate = accumulate, a.whole_sectors = !(((uintptr_t)n.dtable | a.dtable_stride) & 31u);
     a.parts = n.tokens > kRunPart ? (unsigned)((n.tokens + kRunPart - 1) / kRunPart) : 0u;
+    a.rows = (unsigned)(accumulate ? n.tokens : n.vocab_rows);
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const auto run = [&](auto rows, auto join, int per_thread) {
@@ -366,18 +410,24 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
             a.group = sh.group, a.chunks = sh.chunks;
             const unsigned groups = 256u / sh.group;
             const auto blocks = [&](unsigned long long units) { return (units + groups - 1) / groups; };
-            a.row_units = (unsigned long long)(accumulate ? n.tokens : n.vocab_rows) * sh.chunks;
-            const unsigned long long part_blocks = blocks(2ull * a.parts * sh.chunks), grid = part_blocks + blocks(a.row_units);
+            // as many rows at once as leave each SM 32 warps' work
+            a.each = 1;
+            while (a.each < 16u && (unsigned long long)a.rows / (2u * a.each) * sh.chunks * (sh.group / 32u) >= 32ull * kSms) a.each *= 2u;
+            const unsigned long long row_units = ((unsigned long long)a.rows + a.each - 1) / a.each * sh.chunks, part_units = (unsigned long long)a.parts * sh.chunks;
+            if (row_units > kMaxUnits || part_units > kMaxUnits) return (int)NUNA_ERR_TOO_LARGE;
+            a.row_units = (unsigned)row_units;
+            a.part_blocks = (unsigned)blocks(part_units);
+            const unsigned long long grid = a.part_blocks + blocks(row_units);
             if (grid > kMaxExtent) return (int)NUNA_ERR_TOO_LARGE;
-            a.part_blocks = (unsigned)part_blocks;
             const int ok = launch_op(rows, Shape{(unsigned)grid, groups * sh.group, 0, 1}, flags, stream, a);
             if (ok != NUNA_OK || a.parts == 0u) return ok;
-            return launch_op(join, Shape{(unsigned)blocks((unsigned long long)a.parts * sh.chunks), groups * sh.group, 0, 1}, flags, stream, a);
+            const size_t most = (size_t)a.parts * ((n.hidden + kJoinColumns - 1) / kJoinColumns);   // there are no more cut runs than parts
+            return launch_op(join, Shape{(unsigned)std::min<size_t>(most, 4 * kSms), 256, 0, 1}, flags, stream, a);
         };
         const auto typed = [&](auto gt) {
             constexpr int GT = decltype(gt)::value;
-            if (vec) return run(k_embedding_rows<DT, GT, 2, true>, k_embedding_join<GT, Elem<DT>::kElems, 2>, 2);
-            return run(k_embedding_rows<DT, GT, 4, false>, k_embedding_join<GT, 1, 4>, 4);
+            if (vec) return run(k_embedding_rows<DT, GT, 2, true>, k_embedding_join<GT>, 2);
+            return run(k_embedding_rows<DT, GT, 4, false>, k_embedding_join<GT>, 4);
         };
         return n.grad_dtype == NUNA_F32 ? typed(std::integral_constant<int, kF32>{}) : typed(dt);
     });

@@ -15,23 +15,23 @@ struct ExpertSortArgs {
     int *row_of_pair, *pair_of_row, *offsets, *counts;
     long long first_expert;
     unsigned pairs, num_experts, capacity, rows;
-    bool wide;
 };
 
+template <typename Id>
 __global__ void __launch_bounds__(1024) k_expert_sort(const ExpertSortArgs a)
 {
     extern __shared__ unsigned smem[];
     pdl_wait();
     unsigned* counts = smem;                                         // [num_experts]
     const unsigned threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
-    const unsigned kept = sort_pass(a.pairs, a.num_experts, smem + a.num_experts, counts,
-        [&](unsigned i) {
-            const long long e = a.wide ? static_cast<const volatile long long*>(a.experts)[i]
-                                       : (long long)static_cast<const volatile int*>(a.experts)[i];
-            if (e < a.first_expert || (unsigned long long)e - (unsigned long long)a.first_expert >= a.num_experts) return kNoDigit;
-            return (unsigned)(e - a.first_expert);
+    const Id* ids = static_cast<const Id*>(a.experts);
+    const unsigned kept = sort_pass<long long>(a.pairs, a.num_experts, smem + a.num_experts, counts,
+        [&](unsigned i) { return load_id(ids + i); },
+        [&](long long e) {
+            const unsigned long long from = (unsigned long long)e - (unsigned long long)a.first_expert;
+            return e >= a.first_expert && from < a.num_experts ? (unsigned)from : kNoDigit;
         },
-        [&](unsigned i, unsigned d, unsigned first, unsigned rank) {
+        [&](unsigned i, long long, unsigned d, unsigned first, unsigned rank) {
             int row = -1;
             if (d != kNoDigit) {
                 if (a.capacity == 0u) row = (int)(first + rank);
@@ -66,48 +66,65 @@ struct MoveArgs {
     void *y, *out;                                                   // token rows (written), expert rows (written)
     float* dweights;
     size_t x_stride, src_stride, y_stride, out_stride;               // bytes
-    unsigned long long token_units, row_units;                       // tokens * chunks, rows * chunks (if empty rows are zeroed)
+    unsigned units, token_blocks;                                    // tokens * chunks; the blocks behind those zero rows that no pair has
     unsigned topk, rows, packs, chunks, group;                       // packs in a row, chunks of a row, threads of a chunk
 };
 
-// Zeroes the chunk of an expert row that no pair has.
-template <int DT, int kPacks, bool kVec>
-__device__ __forceinline__ void zero_empty_row(const MoveArgs& a, unsigned long long unit, unsigned lane)
+constexpr unsigned kZeroRows = 64;                                   // rows that a block looks at
+
+// Zeroes those of the block's kZeroRows expert rows that no pair has.
+template <int DT, bool kVec>
+__device__ __forceinline__ void zero_empty_rows(const MoveArgs& a)
 {
-    const size_t row = unit / a.chunks;
-    if (a.pair_of_row[row] >= 0) return;
-    const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
+    __shared__ unsigned empty[kZeroRows / 32u];
+    const unsigned first = (blockIdx.x - a.token_blocks) * kZeroRows, r = first + threadIdx.x;
+    if (threadIdx.x < kZeroRows) {
+        const unsigned votes = __ballot_sync(0xFFFFFFFFu, r < a.rows && a.pair_of_row[r] < 0);
+        if ((threadIdx.x & 31u) == 0u) empty[threadIdx.x / 32u] = votes;
+    }
+    __syncthreads();
     Pack<DT, kVec> zero;
 #pragma unroll
     for (int w = 0; w < Pack<DT, kVec>::kWords; ++w) zero.w[w] = 0u;
-#pragma unroll
-    for (int k = 0; k < kPacks; ++k)
-        if (from + k * a.group < a.packs) store_pack<DT, kVec, true>(row_at(a.out, row, a.out_stride), from + k * a.group, zero);
+    for (unsigned q = 0; q < kZeroRows / 32u; ++q)
+        for (unsigned left = empty[q]; left; left &= left - 1u) {
+            void* row = row_at(a.out, (size_t)first + q * 32u + __ffs(left) - 1u, a.out_stride);
+            for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) store_pack<DT, kVec, true>(row, i, zero);
+        }
 }
 
 template <int DT, int kPacks, bool kVec>
 __global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
 {
+    constexpr int kAhead = 8;                                        // rows of the map that are fetched together
     pdl_wait();
-    const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
-    if (unit < a.token_units) {
-        const size_t token = unit / a.chunks;
-        const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
-        Pack<DT, kVec> p[kPacks];
-#pragma unroll
-        for (int k = 0; k < kPacks; ++k)
-            if (from + k * a.group < a.packs) p[k] = load_pack<DT, kVec>(row_at(a.x, token, a.x_stride), from + k * a.group);
-        for (unsigned j = 0; j < a.topk; ++j) {
-            const unsigned row = (unsigned)a.row_of_pair[token * a.topk + j];
-            if (row >= a.rows) continue;
-            void* out = row_at(a.out, row, a.out_stride);
+    if (blockIdx.x >= a.token_blocks) {
+        zero_empty_rows<DT, kVec>(a);
+    } else {
+        const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
+        const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+        if (unit < a.units) {
+            const size_t token = unit / a.chunks;
+            const unsigned from = unit % a.chunks * a.group * kPacks + lane;
+            const int* map = a.row_of_pair + token * a.topk;
+            Pack<DT, kVec> p[kPacks];
 #pragma unroll
             for (int k = 0; k < kPacks; ++k)
-                if (from + k * a.group < a.packs) store_pack<DT, kVec, true>(out, from + k * a.group, p[k]);
+                if (from + k * a.group < a.packs) p[k] = load_pack<DT, kVec>(row_at(a.x, token, a.x_stride), from + k * a.group);
+            for (unsigned j0 = 0; j0 < a.topk; j0 += kAhead) {
+                unsigned row[kAhead];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) row[j] = j0 + j < a.topk ? (unsigned)map[j0 + j] : 0xFFFFFFFFu;
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    if (row[j] >= a.rows) continue;
+                    void* out = row_at(a.out, row[j], a.out_stride);
+#pragma unroll
+                    for (int k = 0; k < kPacks; ++k)
+                        if (from + k * a.group < a.packs) store_pack<DT, kVec, true>(out, from + k * a.group, p[k]);
+                }
+            }
         }
-    } else if (unit - a.token_units < a.row_units) {
-        zero_empty_row<DT, kPacks, kVec>(a, unit - a.token_units, lane);
     }
     pdl_trigger();
 }
@@ -116,13 +133,15 @@ template <int DT, int kPacks, bool kVec>
 __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
-    constexpr int kAhead = 4;                                        // expert rows in flight
+    constexpr int kAhead = kVec && kPacks == 2 ? 4 : 8;              // expert rows in flight
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
-    if (unit < a.token_units) {
+    const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+    if (unit < a.units) {
         const size_t token = unit / a.chunks;
-        const unsigned from = (unsigned)(unit % a.chunks) * a.group * kPacks + lane;
+        const unsigned from = unit % a.chunks * a.group * kPacks + lane;
+        const int* map = a.row_of_pair + token * a.topk;
+        const float* weights = a.weights ? a.weights + token * a.topk : nullptr;
         float acc[kPacks][E];
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
@@ -130,9 +149,13 @@ __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
             for (int e = 0; e < E; ++e) acc[k][e] = 0.0f;
         for (unsigned j0 = 0; j0 < a.topk; j0 += kAhead) {
             unsigned row[kAhead];
+            float w[kAhead];
             Pack<DT, kVec> v[kAhead][kPacks];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) row[j] = j0 + j < a.topk ? (unsigned)a.row_of_pair[token * a.topk + j0 + j] : 0xFFFFFFFFu;
+            for (int j = 0; j < kAhead; ++j) {
+                row[j] = j0 + j < a.topk ? (unsigned)map[j0 + j] : 0xFFFFFFFFu;
+                w[j] = weights && j0 + j < a.topk ? weights[j0 + j] : 1.0f;
+            }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
                 if (row[j] < a.rows)
@@ -141,17 +164,15 @@ __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
                         if (from + k * a.group < a.packs) v[j][k] = load_pack<DT, kVec>(row_at(a.src, row[j], a.src_stride), from + k * a.group);
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
-                if (row[j] < a.rows) {
-                    const float w = a.weights ? a.weights[token * a.topk + j0 + j] : 1.0f;
+                if (row[j] < a.rows)
 #pragma unroll
                     for (int k = 0; k < kPacks; ++k)
                         if (from + k * a.group < a.packs) {
                             float f[E];
                             unpack<DT, kVec>(f, v[j][k]);
 #pragma unroll
-                            for (int e = 0; e < E; ++e) acc[k][e] = fmaf(w, f[e], acc[k][e]);
+                            for (int e = 0; e < E; ++e) acc[k][e] = fmaf(w[j], f[e], acc[k][e]);
                         }
-                }
         }
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
@@ -163,26 +184,28 @@ __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
 // A token per group of threads, which goes over the row kPacks packs a thread at a time; kBatch pairs' products are summed
 // together, and over the group at the end of the row.
 template <int DT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs a)
+__global__ void __launch_bounds__(512) k_expert_combine_backward(const MoveArgs a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
     constexpr int kBatch = 4;
-    __shared__ float red[8][kBatch];
+    __shared__ float red[2][16][kBatch];
     pdl_wait();
-    const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group, warps = a.group / 32u;
-    const unsigned long long unit = (unsigned long long)blockIdx.x * groups + threadIdx.x / a.group;
-    const unsigned long long first = (unsigned long long)blockIdx.x * groups;
-    const size_t token = unit;
-    const bool live = unit < a.token_units;
-    if (first < a.token_units) {                                     // the whole block: the sums exchange through shared memory
-        for (unsigned j0 = 0; j0 < a.topk; j0 += kBatch) {
+    if (blockIdx.x >= a.token_blocks) {
+        zero_empty_rows<DT, kVec>(a);
+    } else {
+        const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group, warps = a.group / 32u;
+        const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+        const size_t token = unit;
+        const bool live = unit < a.units;
+        unsigned turn = 0;
+        for (unsigned j0 = 0; j0 < a.topk; j0 += kBatch, turn ^= 1u) {
             unsigned row[kBatch];
             float w[kBatch], dot[kBatch];
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 const bool is = live && j0 + j < a.topk;
                 row[j] = is ? (unsigned)a.row_of_pair[token * a.topk + j0 + j] : 0xFFFFFFFFu;
-                w[j] = is && row[j] < a.rows ? a.weights[token * a.topk + j0 + j] : 0.0f;
+                w[j] = is ? a.weights[token * a.topk + j0 + j] : 0.0f;
                 dot[j] = 0.0f;
             }
             for (unsigned base = lane; base < a.packs; base += a.group * kPacks) {
@@ -223,14 +246,13 @@ __global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs 
                 warp_sum<kBatch>(dot);
                 if (warps > 1u) {
                     const unsigned warp = threadIdx.x >> 5;
-                    __syncthreads();                                 // the last batch's sums have been read
                     if ((threadIdx.x & 31u) == 0u)
 #pragma unroll
-                        for (int j = 0; j < kBatch; ++j) red[warp][j] = dot[j];
-                    __syncthreads();
+                        for (int j = 0; j < kBatch; ++j) red[turn][warp][j] = dot[j];
+                    __syncthreads();                                 // the next batch has the other half of `red`
                     if (lane < kBatch) {
                         float s = 0.0f;
-                        for (unsigned o = 0; o < warps; ++o) s += red[warp + o][lane];
+                        for (unsigned o = 0; o < warps; ++o) s += red[turn][warp + o][lane];
                         if (live && j0 + lane < a.topk) a.dweights[token * a.topk + j0 + lane] = s;
                     }
                 } else if (live && lane == 0u) {
@@ -241,38 +263,30 @@ __global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs 
             }
         }
     }
-    if (!live) {
-        // the groups that have no token zero the rows that have no pair, a chunk at a time
-        const unsigned long long z = unit - a.token_units;
-        if (z < a.row_units) zero_empty_row<DT, kPacks, kVec>(a, z, lane);
-    }
     pdl_trigger();
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
 
-// Threads (at most 256) and chunks for a row of `packs` packs, kPacks a thread.
-static void row_shape(MoveArgs& a, int per_thread)
-{
-    const unsigned threads = (a.packs + per_thread - 1) / per_thread;
-    a.group = std::max(32u, std::min(256u, (threads + 31u) / 32u * 32u));
-    a.chunks = std::max(1u, (threads + a.group - 1) / a.group);
-}
-
 static size_t stride_bytes(size_t stride, size_t hidden, int dtype) { return (stride ? stride : hidden) * dtype_bytes(dtype); }
 
-// Launches a row mover: `whole` says that a group takes a token's row whole, not a chunk of it.
+// Launches a row mover with kPacks packs a thread in groups of at most `most` threads, which take chunks of a row, or (`whole`)
+// a row in several steps.
 template <typename Kernel>
-static int move_rows(Kernel kernel, MoveArgs& a, size_t tokens, int per_thread, bool whole, unsigned flags, void* stream)
+static int move_rows(Kernel kernel, MoveArgs& a, size_t tokens, int per_thread, unsigned most, bool whole, unsigned flags, void* stream)
 {
-    row_shape(a, per_thread);
-    a.token_units = (unsigned long long)tokens * (whole ? 1u : a.chunks);
-    a.row_units = a.pair_of_row ? (unsigned long long)a.rows * a.chunks : 0u;
-    const unsigned groups = 256u / a.group;
-    const unsigned long long grid = (a.token_units + a.row_units + groups - 1) / groups;
+    const unsigned threads = (a.packs + per_thread - 1) / per_thread, steps = std::max(1u, (threads + most - 1) / most);
+    a.group = std::max(32u, ((threads + steps - 1) / steps + 31u) / 32u * 32u);          // steps of about the same length
+    a.chunks = whole ? 1u : steps;
+    const unsigned groups = std::max(1u, 256u / a.group);
+    const unsigned long long units = (unsigned long long)tokens * a.chunks;
+    if (units > 0xFFFFFF00ull) return NUNA_ERR_TOO_LARGE;            // 32 bits count the units
+    a.units = (unsigned)units;
+    a.token_blocks = (unsigned)((units + groups - 1) / groups);
+    const unsigned long long grid = a.token_blocks + (a.pair_of_row ? (a.rows + kZeroRows - 1ull) / kZeroRows : 0ull);
     if (grid > kMaxExtent) return NUNA_ERR_TOO_LARGE;
     if (grid == 0) return NUNA_OK;
-    return launch_op(kernel, Shape{(unsigned)grid, groups * a.group, 0, 1}, flags, stream, a);
+    return launch_op(kernel, Shape{(unsigned)grid, std::max(kZeroRows, groups * a.group), 0, 1}, flags, stream, a);
 }
 
 static int dispatch(const nuna_expert_dispatch_t& n, unsigned flags, void* stream)
@@ -286,11 +300,11 @@ static int dispatch(const nuna_expert_dispatch_t& n, unsigned flags, void* strea
     const size_t tokens = n.topk ? n.tokens : 0;
     if (vec) {                                                       // bits are copied: a vector is a vector
         return (unsigned long long)tokens * a.packs <= 4ull * kSms * 512ull
-                   ? move_rows(k_expert_dispatch<kF32, 1, true>, a, tokens, 1, false, flags, stream)
-                   : move_rows(k_expert_dispatch<kF32, 4, true>, a, tokens, 4, false, flags, stream);
+                   ? move_rows(k_expert_dispatch<kF32, 1, true>, a, tokens, 1, 256, false, flags, stream)
+                   : move_rows(k_expert_dispatch<kF32, 4, true>, a, tokens, 4, 256, false, flags, stream);
     }
-    if (n.dtype == NUNA_F32) return move_rows(k_expert_dispatch<kF32, 4, false>, a, tokens, 4, false, flags, stream);
-    return move_rows(k_expert_dispatch<kBf16, 4, false>, a, tokens, 4, false, flags, stream);
+    if (n.dtype == NUNA_F32) return move_rows(k_expert_dispatch<kF32, 4, false>, a, tokens, 4, 256, false, flags, stream);
+    return move_rows(k_expert_dispatch<kBf16, 4, false>, a, tokens, 4, 256, false, flags, stream);
 }
 
 static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
@@ -303,10 +317,10 @@ static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
     a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine<DT, 4, false>, a, n.tokens, 4, false, flags, stream);
+        if (!vec) return move_rows(k_expert_combine<DT, 4, false>, a, n.tokens, 4, 256, false, flags, stream);
         return (unsigned long long)n.tokens * a.packs <= 2ull * kSms * 512ull
-                   ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, false, flags, stream)
-                   : move_rows(k_expert_combine<DT, 2, true>, a, n.tokens, 2, false, flags, stream);
+                   ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, 256, false, flags, stream)
+                   : move_rows(k_expert_combine<DT, 2, true>, a, n.tokens, 2, 256, false, flags, stream);
     });
 }
 
@@ -324,8 +338,8 @@ static int combine_backward(const nuna_expert_combine_grad_t& n, unsigned flags,
     const size_t tokens = n.topk ? n.tokens : 0;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine_backward<DT, 4, false>, a, tokens, 4, true, flags, stream);
-        return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, true, flags, stream);
+        if (!vec) return move_rows(k_expert_combine_backward<DT, 4, false>, a, tokens, 4, 512, true, flags, stream);
+        return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, 256, true, flags, stream);
     });
 }
 
@@ -345,14 +359,14 @@ int nuna_expert_sort(const nuna_expert_sort_t* args, unsigned flags, void* strea
     if (st != NUNA_OK) return st;
     const size_t pairs = a.tokens * a.topk, rows = a.capacity ? a.num_experts * a.capacity : pairs;
     const ExpertSortArgs k = {a.experts, a.row_of_pair, a.pair_of_row, a.offsets, a.counts, a.first_expert, (unsigned)pairs,
-                              (unsigned)a.num_experts, (unsigned)a.capacity, (unsigned)rows, a.id_bytes == 8};
+                              (unsigned)a.num_experts, (unsigned)a.capacity, (unsigned)rows};
     Shape s = sort_shape(pairs, k.num_experts);
     s.smem += k.num_experts * 4u;
-    if (s.smem > 32 * 1024) {
-        const int ok = allow_smem<k_expert_sort>(sort_smem(kSortMaxWarps, NUNA_MAX_EXPERTS) + NUNA_MAX_EXPERTS * 4);
-        if (ok != NUNA_OK) return ok;
-    }
-    return launch_op(k_expert_sort, s, effective_flags(flags, stream), stream, k);
+    constexpr int kMost = sort_smem(kSortMaxWarps, NUNA_MAX_EXPERTS) + NUNA_MAX_EXPERTS * 4;
+    const bool wide = a.id_bytes == 8;
+    const int ok = s.smem <= 32 * 1024 ? NUNA_OK : wide ? allow_smem<k_expert_sort<long long>>(kMost) : allow_smem<k_expert_sort<int>>(kMost);
+    if (ok != NUNA_OK) return ok;
+    return launch_op(wide ? k_expert_sort<long long> : k_expert_sort<int>, s, effective_flags(flags, stream), stream, k);
 }
 
 int nuna_expert_dispatch(const nuna_expert_dispatch_t* args, unsigned flags, void* stream)

@@ -152,6 +152,14 @@ __device__ __forceinline__ void store_pack(void* row, size_t i, const Pack<DT, k
     }
 }
 
+// 32 bytes at a 32-byte address in one store: a warp whose lanes hold eight binary32 each writes whole sectors, which two
+// 16-byte stores do not (they reach L2 as halves of twice as many).
+__device__ __forceinline__ void store8(float* p, const float (&f)[8])
+{
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+}
+
 template <int DT, bool kVec>
 __device__ __forceinline__ void unpack(float (&f)[Pack<DT, kVec>::kElems], const Pack<DT, kVec>& p)
 {

@@ -16,8 +16,11 @@ constexpr unsigned kSortMaxWarps = 32;
 constexpr unsigned kSortMaxCluster = 8;
 constexpr unsigned kNoDigit = 0xFFFFFFFFu;
 
-// Dynamic shared memory of a pass over `bins` bins: [warps][bins] counts, [bins] totals, [bins] first places.
-__host__ __device__ constexpr unsigned sort_smem(unsigned warps, unsigned bins) { return (warps + 2u) * bins * 4u; }
+constexpr unsigned kSortSegments = 8;                    // cuts of a bin's counts by warp
+
+// Dynamic shared memory of a pass over `bins` bins: [warps][bins] counts, [bins] totals, [bins] first places, [bins] items of
+// earlier blocks, [segments][bins] sums.
+__host__ __device__ constexpr unsigned sort_smem(unsigned warps, unsigned bins) { return (warps + 3u + kSortSegments) * bins * 4u; }
 
 __device__ __forceinline__ unsigned ld_shared_of(const unsigned* local_ptr, unsigned cta)
 {
@@ -51,105 +54,159 @@ __device__ __forceinline__ unsigned block_exclusive_sum(unsigned v, unsigned* re
     return s - v + __shfl_sync(0xFFFFFFFFu, t - w, warp);
 }
 
-// One pass over items 0 ... n-1.  digit(i): the item's bin or kNoDigit (dropped); it is asked twice if a warp has more than
-// 32 * kSortItems items.  place(i, digit, first, rank): called once for every item, in any order; `first` is where its bin
-// begins, `rank` its number within the bin.  count(bin): with `counts` (shared, [bins]) given, what all blocks have of a bin.
-// Returns the number of items that were not dropped.  All threads of the cluster call; shared memory may be reused, and what
-// place() wrote to global memory is visible to the whole cluster, when it returns.
-template <typename Digit, typename Place>
-__device__ __forceinline__ unsigned sort_pass(unsigned n, unsigned bins, unsigned* smem, unsigned* counts, Digit digit, Place place)
+// Ids of the caller's, and what blocks of this kernel have written for one another, without waiting for the one before.
+__device__ __forceinline__ long long load_id(const long long* p)
+{
+    long long v;
+    asm volatile("ld.global.s64 %0, [%1];" : "=l"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ long long load_id(const int* p) { return (int)ld_src32(reinterpret_cast<const uint32_t*>(p)); }
+__device__ __forceinline__ uint2 load_shared_by_cluster(const uint2* p)
+{
+    uint2 v;
+    asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+
+// All threads of the cluster.
+__device__ __forceinline__ void sort_sync(unsigned blocks)
+{
+    if (blocks == 1u) __syncthreads();
+    else              cluster_sync();
+}
+
+// One pass over items 0 ... n-1.  load(i): the item (asked twice if a warp has more than 32 * kSortItems of them);
+// digit(item): its bin, or kNoDigit to drop it; place(i, item, digit, first, rank): called once for every item, in any
+// order; `first` is where its bin begins, `rank` its number within the bin.  `counts` (shared, [bins]), if given, receives what
+// all blocks have of each bin.  Returns the number of items that were not dropped.  All threads of the cluster call; shared
+// memory may be reused, and what place() wrote to global memory is visible to the whole cluster, when it returns.
+template <typename Item, typename Load, typename Digit, typename Place>
+__device__ __forceinline__ unsigned sort_pass(unsigned n, unsigned bins, unsigned* smem, unsigned* counts, Load load, Digit digit, Place place)
 {
     __shared__ unsigned red[32];
     const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const unsigned blocks = gridDim.x, block = blockIdx.x;                       // the grid is the cluster
-    unsigned *hist = smem, *totals = smem + warps * bins, *first = totals + bins;
+    unsigned *hist = smem, *totals = hist + warps * bins, *first = totals + bins, *ahead = first + bins, *segment = ahead + bins;
     const unsigned parts = blocks * warps;
     const unsigned per_warp = (unsigned)(((unsigned long long)n + parts * 32ull - 1ull) / (parts * 32ull) * 32ull);
     const unsigned long long at = (unsigned long long)(block * warps + warp) * per_warp;
     const unsigned begin = (unsigned)(at < n ? at : n), end = (unsigned)(at + per_warp < n ? at + per_warp : n);
     const bool kept = per_warp <= 32u * kSortItems;
     unsigned* mine = hist + warp * bins;
-    unsigned d[kSortItems];
+    Item item[kSortItems];
+    unsigned held[kSortItems];                           // an item's number among its warp's items of its digit
 
+    const auto fetch = [&](unsigned base) {
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k)
+            if (base + k * 32u + lane < end) item[k] = load(base + k * 32u + lane);
+    };
+    if (kept) fetch(begin);
     for (unsigned b = threadIdx.x; b < warps * bins; b += blockDim.x) hist[b] = 0u;
     __syncthreads();
     for (unsigned base = begin; base < end; base += 32u * kSortItems) {
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const unsigned i = base + k * 32u + lane;
-            d[k] = i < end ? digit(i) : kNoDigit;
-        }
+        if (!kept) fetch(base);
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
             if (base + k * 32u >= end) break;
-            const unsigned peers = __match_any_sync(0xFFFFFFFFu, d[k]);
-            if (d[k] != kNoDigit && lane == (unsigned)__ffs(peers) - 1u) mine[d[k]] += __popc(peers);
+            const unsigned d = base + k * 32u + lane < end ? digit(item[k]) : kNoDigit;
+            const unsigned peers = __match_any_sync(0xFFFFFFFFu, d), before = d != kNoDigit ? mine[d] : 0u;
+            held[k] = before + __popc(peers & ((1u << lane) - 1u));
+            __syncwarp();
+            if (d != kNoDigit && lane == (unsigned)__ffs(peers) - 1u) mine[d] = before + __popc(peers);
             __syncwarp();
         }
     }
     __syncthreads();
-    for (unsigned b = threadIdx.x; b < bins; b += blockDim.x) {
+    // What a bin has in earlier warps, and in all: a bin's warps are cut into segments, summed by a thread each.
+    unsigned segments = 1;
+    while (segments < kSortSegments && segments * 2u <= warps && segments * 2u * bins <= blockDim.x) segments *= 2u;
+    const unsigned each = (warps + segments - 1u) / segments;
+    for (unsigned t = threadIdx.x; t < segments * bins; t += blockDim.x) {
+        const unsigned q = t / bins, b = t - q * bins;
+        unsigned sum = 0;
+        for (unsigned w = q * each; w < warps && w < (q + 1u) * each; ++w) sum += hist[w * bins + b];
+        segment[t] = sum;
+    }
+    __syncthreads();
+    for (unsigned t = threadIdx.x; t < segments * bins; t += blockDim.x) {
+        const unsigned q = t / bins, b = t - q * bins;
         unsigned run = 0;
-        for (unsigned w = 0; w < warps; ++w) {
+        for (unsigned o = 0; o < q; ++o) run += segment[o * bins + b];
+        for (unsigned w = q * each; w < warps && w < (q + 1u) * each; ++w) {
             const unsigned c = hist[w * bins + b];
             hist[w * bins + b] = run;
             run += c;
         }
-        totals[b] = run;
+        if (q == segments - 1u) totals[b] = run;
     }
-    cluster_sync();
+    sort_sync(blocks);
     unsigned carry = 0;
     for (unsigned b0 = 0; b0 < bins; b0 += blockDim.x) {
         const unsigned b = b0 + threadIdx.x;
         unsigned before = 0, all = 0;
-        if (b < bins)
-            for (unsigned c = 0; c < blocks; ++c) {
-                const unsigned v = blocks == 1u ? totals[b] : ld_shared_of(totals + b, c);
-                if (c < block) before += v;
-                all += v;
+        if (b < bins) {
+            if (blocks == 1u) {
+                all = totals[b];
+            } else {
+                unsigned v[kSortMaxCluster];
+#pragma unroll
+                for (unsigned c = 0; c < kSortMaxCluster; ++c) v[c] = c < blocks ? ld_shared_of(totals + b, c) : 0u;
+#pragma unroll
+                for (unsigned c = 0; c < kSortMaxCluster; ++c) {
+                    before += c < block ? v[c] : 0u;
+                    all += v[c];
+                }
             }
+        }
         unsigned total;
         const unsigned sum = block_exclusive_sum(all, red, total);
         if (b < bins) {
             first[b] = carry + sum;
+            ahead[b] = before;
             if (counts) counts[b] = all;
-            for (unsigned w = 0; w < warps; ++w) hist[w * bins + b] += before;
         }
         carry += total;
     }
     __syncthreads();
-    for (unsigned base = begin; base < end; base += 32u * kSortItems) {
-        if (!kept) {
-#pragma unroll
-            for (int k = 0; k < kSortItems; ++k) {
-                const unsigned i = base + k * 32u + lane;
-                d[k] = i < end ? digit(i) : kNoDigit;
-            }
-        }
+    if (kept) {
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k) {
-            if (base + k * 32u >= end) break;
-            const unsigned i = base + k * 32u + lane, peers = __match_any_sync(0xFFFFFFFFu, d[k]);
-            unsigned rank = 0;
-            if (d[k] != kNoDigit) rank = mine[d[k]] + __popc(peers & ((1u << lane) - 1u));
-            __syncwarp();
-            if (d[k] != kNoDigit && lane == (unsigned)__ffs(peers) - 1u) mine[d[k]] += __popc(peers);
-            __syncwarp();
-            if (i < end) place(i, d[k], d[k] != kNoDigit ? first[d[k]] : 0u, rank);
+            const unsigned i = begin + k * 32u + lane;
+            if (i >= end) break;
+            const unsigned d = digit(item[k]);
+            if (d == kNoDigit) place(i, item[k], d, 0u, 0u);
+            else               place(i, item[k], d, first[d], ahead[d] + mine[d] + held[k]);
+        }
+    } else {
+        for (unsigned base = begin; base < end; base += 32u * kSortItems) {
+            fetch(base);
+#pragma unroll
+            for (int k = 0; k < kSortItems; ++k) {
+                if (base + k * 32u >= end) break;
+                const unsigned i = base + k * 32u + lane, d = i < end ? digit(item[k]) : kNoDigit;
+                const unsigned peers = __match_any_sync(0xFFFFFFFFu, d), before = d != kNoDigit ? mine[d] : 0u;
+                __syncwarp();
+                if (d != kNoDigit && lane == (unsigned)__ffs(peers) - 1u) mine[d] = before + __popc(peers);
+                __syncwarp();
+                if (i < end) place(i, item[k], d, d != kNoDigit ? first[d] : 0u, d != kNoDigit ? ahead[d] + before + __popc(peers & ((1u << lane) - 1u)) : 0u);
+            }
         }
     }
-    cluster_sync();
+    sort_sync(blocks);
     return carry;
 }
 
-// Blocks of the cluster and warps of a block that sort n items: a warp takes 32 * kSortItems items before there are more of them.
+// Blocks of the cluster and warps of a block that sort n items.  One block takes up to kSortAlone: beyond, eight of them are
+// ahead of what their barriers cost.
+constexpr size_t kSortAlone = 4096;
+constexpr size_t kSortEach = 4;                          // items of a lane for which another warp is not worth its part in the sums
 inline Shape sort_shape(size_t n, unsigned bins)
 {
-    const size_t warps = (n + 32 * kSortItems - 1) / (32 * kSortItems);
-    unsigned cluster = 1;
-    while (cluster < kSortMaxCluster && cluster * kSortMaxWarps < warps) cluster *= 2;
-    unsigned per_block = (unsigned)((warps + cluster - 1) / cluster);
-    per_block = per_block < 4u ? 4u : per_block > kSortMaxWarps ? kSortMaxWarps : per_block;
+    const unsigned cluster = n <= kSortAlone ? 1u : kSortMaxCluster;
+    const size_t warps = (n / cluster + 32 * kSortEach - 1) / (32 * kSortEach);
+    const unsigned per_block = (unsigned)(warps < 4 ? 4 : warps > kSortMaxWarps ? kSortMaxWarps : warps);
     return Shape{cluster, per_block * 32u, sort_smem(per_block, bins), cluster};
 }
 

@@ -67,12 +67,13 @@ inline size_t layernorm_workspace_bytes(size_t rows, size_t hidden)
     return norm_blocks(rows) * 2 * ((hidden + 3) / 4 * 4) * sizeof(float);
 }
 
-// Embedding: the tokens in the order of their ids (two buffers of tokens and two of ids, between which the sort's passes
-// alternate), where each row's run of tokens begins and ends, how many tokens have a row, and the shares of runs that
-// are cut: two rows for every kRunPart positions.
-constexpr size_t kRunPart = 64;
+// Embedding: the tokens with their rows, in the order of the rows (two buffers, between which the sort's passes alternate),
+// where each row's run of tokens begins and ends, how many tokens have a row and how many runs are cut, which those are, and
+// their shares: two rows for every kRunPart positions.
+constexpr size_t kRunPart = 32;
+inline size_t part_stride(size_t hidden) { return (hidden + 7) / 8 * 8; }
 struct EmbeddingWorkspace {
-    size_t token[2], id[2], begin, end, count, part, bytes;
+    size_t items[2], begin, end, count, cut, part, bytes;
 };
 inline EmbeddingWorkspace embedding_workspace(size_t tokens, size_t hidden, size_t vocab_rows)
 {
@@ -83,9 +84,10 @@ inline EmbeddingWorkspace embedding_workspace(size_t tokens, size_t hidden, size
         w.bytes += (n * 4 + 255) / 256 * 256;
         return at;
     };
-    w.token[0] = take(tokens), w.token[1] = take(tokens), w.id[0] = take(tokens), w.id[1] = take(tokens);
-    w.begin = take(vocab_rows), w.end = take(vocab_rows), w.count = take(1);
-    w.part = take(tokens > kRunPart ? (tokens + kRunPart - 1) / kRunPart * 2 * ((hidden + 3) / 4 * 4) : 0);
+    w.items[0] = take(2 * tokens), w.items[1] = take(2 * tokens);
+    w.begin = take(vocab_rows), w.end = take(vocab_rows), w.count = take(2);
+    w.cut = take(tokens > kRunPart ? tokens / kRunPart : 0);
+    w.part = take(tokens > kRunPart ? (tokens + kRunPart - 1) / kRunPart * 2 * part_stride(hidden) : 0);
     return w;
 }
 

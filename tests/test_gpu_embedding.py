@@ -81,9 +81,9 @@ def run_backward(tokens, hidden, rows, start, vocab, dtype, grad, kind, scale=0.
         total = want + old.double() if accumulate else want
         assert torch.equal(dtable.v.double(), total.to(gdt).double()), what
     else:
-        # at most 64 additions in a part and as many as there are parts, of values whose absolute sum is `size`
+        # at most 32 additions in a part and as many as there are parts, of values whose absolute sum is `size`
         size = torch.zeros_like(want).index_add_(0, at[mine], dout.v[mine].double().abs()) * scale
-        bound = (64 + tokens // 64 + 4) * U * size
+        bound = (32 + tokens // 32 + 4) * U * size
         within(dtable.v, want, bound + half_step(gdt) * (want.abs() + bound) + smallest(gdt), what)
     if accumulate:
         present = torch.zeros(rows, dtype=torch.bool, device="cuda").index_fill_(0, at[mine], True)
@@ -104,7 +104,7 @@ def test_backward(shape, dtype, grad):
         run_backward(*shape, dtype, grad, "i32", pad=pad, shift=shift, accumulate=True)
 
 
-@pytest.mark.parametrize("tokens", [1, 2, 63, 64, 65, 127, 128, 129, 191, 1000, 4096])
+@pytest.mark.parametrize("tokens", [1, 2, 31, 32, 33, 63, 64, 65, 96, 97, 127, 128, 129, 191, 1000, 4096])
 def test_all_tokens_are_one_id(tokens):
     for same in (0, 6):
         run_backward(tokens, 48, 7, 0, 7, "bf16", "f32", "i64", same=same)
@@ -114,7 +114,8 @@ def test_all_tokens_are_one_id(tokens):
     run_backward(tokens, 48, 7, 0, 7, "bf16", "f32", "i64", same=7, accumulate=True)
 
 
-@pytest.mark.parametrize("lengths", [[64, 64, 64], [65, 63, 64], [1, 64, 65, 1], [63, 65, 128], [200, 1, 1, 1, 70, 64, 129], [32, 65, 31, 65]])
+@pytest.mark.parametrize("lengths", [[64, 64, 64], [65, 63, 64], [1, 64, 65, 1], [63, 65, 128], [200, 1, 1, 1, 70, 64, 129], [32, 65, 31, 65],
+                                     [32, 32, 33], [33, 31, 32, 33, 1, 30], [1, 33, 33, 33], [5, 32, 33, 26, 33], [500, 31, 33, 900]])
 def test_runs_that_end_inside_and_between_the_parts(lengths):
     """Runs of given lengths, in the order of their ids: cut and whole ones, at and around the places where runs are cut."""
     ids = torch.cat([torch.full((n,), i) for i, n in enumerate(lengths)]).cuda()

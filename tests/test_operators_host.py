@@ -149,8 +149,8 @@ def test_workspaces_of_impossible_sizes():
     assert nb.nuna_layernorm_workspace(HUGE, 64) == 0 and nb.nuna_layernorm_workspace(4, HUGE) == 0
     assert nb.nuna_layernorm_workspace(0, 64) == 0
     assert nb.nuna_embedding_workspace(HUGE, 64, 16) == 0 and nb.nuna_embedding_workspace(4, 64, HUGE) == 0
-    # the parts of cut runs: none up to 64 tokens, two rows of binary32 for every 64 tokens beyond
-    assert nb.nuna_embedding_workspace(65, 64, 16) - nb.nuna_embedding_workspace(64, 64, 16) >= 4 * 64 * 4
+    # the parts of cut runs: none up to 32 tokens, two rows of binary32 for every 32 tokens beyond
+    assert nb.nuna_embedding_workspace(33, 64, 16) - nb.nuna_embedding_workspace(32, 64, 16) >= 4 * 64 * 4
     big = nb.nuna_embedding_workspace(HUGE - 1, HUGE - 1, HUGE - 1)
     assert big > 1 << 56                                             # not wrapped
 

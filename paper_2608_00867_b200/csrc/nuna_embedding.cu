@@ -17,56 +17,65 @@ struct LookupArgs {
     size_t table_stride, out_stride;                                 // bytes
     long long vocab_start;
     unsigned tokens, units;                                          // units: (tokens / kTokens) * chunks
-    unsigned vocab_rows, packs, chunks, group;                       // packs in a row, chunks of a row, threads of a chunk
+    unsigned vocab_rows, hidden, chunks, group;                      // chunks of a row, threads of a chunk
     float scale;
 };
 
-// One chunk of kTokens tokens' rows per group of threads, kPacks packs a thread and token: the tokens' ids are fetched together,
-// and then all of their packs.
-template <typename Id, int DT, int kTokens, int kPacks, bool kVec>
+// One chunk of kTokens tokens' rows per group of threads, kPacks pieces a thread and token: the tokens' ids are fetched together,
+// and then all of their pieces.
+template <typename Id, int DT, int kTokens, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_embedding_lookup(const LookupArgs a)
 {
-    using V = Lanes<kVec>;
+    constexpr int E = Elem<DT>::kElems;
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
     if (unit < a.units) {
         const unsigned first = unit / a.chunks * kTokens, from = unit % a.chunks * a.group * kPacks + lane;
         long long id[kTokens];
-        Pack<DT, kVec> p[kTokens][kPacks];
+        Piece<DT, kWhole> p[kTokens][kPacks];
+        Source source[kTokens];
+        int s[kTokens];                                              // by how much the output row is behind a boundary
 #pragma unroll
         for (int t = 0; t < kTokens; ++t) id[t] = first + t < a.tokens ? load_id(static_cast<const Id*>(a.ids) + first + t) : -1;
         unsigned found = 0;
 #pragma unroll
         for (int t = 0; t < kTokens; ++t) {
             const unsigned long long row = (unsigned long long)id[t] - (unsigned long long)a.vocab_start;
-            const bool mine = id[t] >= a.vocab_start && row < a.vocab_rows;
-            const void* at = row_at(a.table, (size_t)row, a.table_stride);
-            if (mine) found |= 1u << t;
+            s[t] = kWhole ? 0 : behind<DT, E>(row_at(a.out, (size_t)first + t, a.out_stride));
+            if (id[t] >= a.vocab_start && row < a.vocab_rows) {
+                found |= 1u << t;
+                source[t] = source_of<DT, kWhole>(a.table, row, a.table_stride, a.vocab_rows, a.hidden, s[t]);
 #pragma unroll
-            for (int k = 0; k < kPacks; ++k) {
-#pragma unroll
-                for (int w = 0; w < Pack<DT, kVec>::kWords; ++w) p[t][k].w[w] = 0u;
-                if (mine && from + k * a.group < a.packs) p[t][k] = load_pack<DT, kVec>(at, from + k * a.group);
+                for (int k = 0; k < kPacks; ++k) {
+                    const unsigned i = from + k * a.group;
+                    const int e0 = (int)(i * E) - s[t];
+                    if (touches<E>(e0, a.hidden)) fetch_piece<DT, kWhole>(p[t][k], source[t], i, e0, a.hidden);
+                }
             }
         }
-        if (a.scale == 1.0f) found = 0;                              // nothing to scale; the zeros of no row never are: the scale may be infinite
 #pragma unroll
         for (int t = 0; t < kTokens; ++t) {
             if (first + t >= a.tokens) break;
             void* out = row_at(a.out, (size_t)first + t, a.out_stride);
 #pragma unroll
-            for (int k = 0; k < kPacks; ++k)
-                if (from + k * a.group < a.packs) {
+            for (int k = 0; k < kPacks; ++k) {
+                const int e0 = (int)((from + k * a.group) * E) - s[t];
+                if (touches<E>(e0, a.hidden)) {
+                    Pack<DT, true> v = {};                           // zeros, which are not scaled: the scale may be infinite
                     if (found >> t & 1u) {
-                        V f[kLanes<DT, kVec>];
-                        unpack<DT, kVec>(f, p[t][k]);
+                        v = settle_piece<DT, kWhole>(p[t][k], source[t]);
+                        if (a.scale != 1.0f) {
+                            Two f[E / 2];
+                            unpack<DT, true>(f, v);
 #pragma unroll
-                        for (int e = 0; e < kLanes<DT, kVec>; ++e) f[e] = f[e] * all<V>(a.scale);
-                        p[t][k] = pack<DT, kVec>(f);
+                            for (int e = 0; e < E / 2; ++e) f[e] = f[e] * all<Two>(a.scale);
+                            v = pack<DT, true>(f);
+                        }
                     }
-                    store_pack<DT, kVec>(out, from + k * a.group, p[t][k]);
+                    store_piece<DT, kWhole>(out, a.hidden, e0, v);
                 }
+            }
         }
     }
     pdl_trigger();
@@ -137,87 +146,101 @@ struct TableArgs {
     size_t dout_stride, dtable_stride;                               // bytes
     unsigned rows, row_units, each;                                  // table rows (positions, if accumulating); (rows / each) * chunks
     unsigned parts, part_blocks;                                     // cuts of the positions, blocks that add them
-    unsigned packs, chunks, group, part_stride;
-    unsigned hidden;
+    unsigned tokens, hidden, chunks, group, part_stride;
     float scale;
     bool accumulate, whole_sectors;                                  // rows of dtable are at 32-byte addresses
 };
 
-// acc += the packs from + k * group of the rows of dout that positions p ... end-1 name, in their order.  A warp fetches 32
-// positions' tokens at once, and then kAhead rows.  All lanes of a warp have the same run.
-template <int DT, int kPacks, bool kVec>
-__device__ __forceinline__ void add_run(float (&acc)[kPacks][Pack<DT, kVec>::kElems], const TableArgs& a, unsigned p, unsigned end, unsigned from)
+// acc += pieces from + k * group, which begin at E times that minus s, of the rows of dout that positions p ... end-1 name, in
+// their order.  A warp fetches 32 positions' tokens at once, and then kAhead rows.  All lanes of a warp have the same run.
+template <int DT, int kPacks, bool kWhole>
+__device__ __forceinline__ void add_run(Two (&acc)[kPacks][Elem<DT>::kElems / 2], const TableArgs& a, unsigned p, unsigned end, unsigned from, int s)
 {
-    constexpr int E = Pack<DT, kVec>::kElems;
-    constexpr int kAhead = kVec ? 4 : 8;
+    constexpr int E = Elem<DT>::kElems;
+    constexpr int kAhead = 4;
     for (; p < end; p += 32u) {
         const unsigned lane = threadIdx.x & 31u, n = end - p < 32u ? end - p : 32u;
         const unsigned token = lane < n ? a.items[p + lane].x : 0u;
         for (unsigned r0 = 0; r0 < n; r0 += kAhead) {
-            Pack<DT, kVec> v[kAhead][kPacks];
+            Piece<DT, kWhole> v[kAhead][kPacks];
+            Source source[kAhead];
 #pragma unroll
             for (int r = 0; r < kAhead; ++r) {
-                const void* row = row_at(a.dout, __shfl_sync(0xFFFFFFFFu, token, r0 + r), a.dout_stride);
+                source[r] = source_of<DT, kWhole>(a.dout, __shfl_sync(0xFFFFFFFFu, token, r0 + r), a.dout_stride, a.tokens, a.hidden, s);
                 if (r0 + r < n)
 #pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (from + k * a.group < a.packs) v[r][k] = load_pack<DT, kVec>(row, from + k * a.group);
+                    for (int k = 0; k < kPacks; ++k) {
+                        const int e0 = (int)((from + k * a.group) * E) - s;
+                        if (touches<E>(e0, a.hidden)) fetch_piece<DT, kWhole>(v[r][k], source[r], from + k * a.group, e0, a.hidden);
+                    }
             }
 #pragma unroll
             for (int r = 0; r < kAhead; ++r)
                 if (r0 + r < n)
 #pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (from + k * a.group < a.packs) {
-                            float f[E];
-                            unpack<DT, kVec>(f, v[r][k]);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) acc[k][e] += f[e];
-                        }
+                    for (int k = 0; k < kPacks; ++k) add_pack<DT, true>(acc[k], settle_piece<DT, kWhole>(v[r][k], source[r]));
         }
     }
 }
 
-// E values of dtable's type GT from element i * E of a row on: rne(scale * sum), or added to what is there.
-template <int GT, int E>
-__device__ __forceinline__ void put_gradient(const TableArgs& a, void* row, unsigned i, float (&sum)[E])
+// E values of dtable's type GT from element e0 of a row on: rne(scale * sum), or added to what is there.
+template <int GT, int E, bool kWhole>
+__device__ __forceinline__ void put_gradient(const TableArgs& a, void* row, int e0, const Two (&acc)[E / 2])
 {
-    constexpr bool kVec = E > 1;
-    constexpr int G = Pack<GT, kVec>::kElems, kParts = E / G;
+    float sum[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = e % 2 ? acc[e / 2].y : acc[e / 2].x;
+    if (!kWhole && !inside<E>(e0, a.hidden)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e0 + e >= 0 && e0 + e < (int)a.hidden) {
+                float f[1] = {sum[e] * a.scale};
+                if (a.accumulate) {
+                    float old[1];
+                    unpack<GT, false>(old, load_pack<GT, false>(row, (size_t)(e0 + e)));
+                    f[0] = __fadd_rn(old[0], f[0]);
+                }
+                store_pack<GT, false>(row, (size_t)(e0 + e), pack<GT, false>(f));
+            }
+        return;
+    }
+    constexpr int G = Elem<GT>::kElems, kParts = E / G;
+    void* at = static_cast<char*>(row) + (long long)e0 * Elem<GT>::kBytes;
 #pragma unroll
     for (int q = 0; q < kParts; ++q) {
         float old[G];
-        if (a.accumulate) unpack<GT, kVec>(old, load_pack<GT, kVec>(row, (size_t)i * kParts + q));
+        if (a.accumulate) unpack<GT, true>(old, load_pack<GT, true>(at, q));
 #pragma unroll
         for (int e = 0; e < G; ++e) {
             sum[q * G + e] *= a.scale;
             if (a.accumulate) sum[q * G + e] = __fadd_rn(old[e], sum[q * G + e]);
         }
     }
+    bool done = false;
     if constexpr (GT == kF32 && E == 8) {
-        if (a.whole_sectors) {
-            store8(static_cast<float*>(row) + (size_t)i * 8u, sum);
-            return;
-        }
+        done = !kWhole || a.whole_sectors;
+        if (done) store8(static_cast<float*>(at), sum);          // pieces of eight are cut at 32-byte boundaries
     }
+    if (!done) {
 #pragma unroll
-    for (int q = 0; q < kParts; ++q) {
-        float f[G];
+        for (int q = 0; q < kParts; ++q) {
+            float f[G];
 #pragma unroll
-        for (int e = 0; e < G; ++e) f[e] = sum[q * G + e];
-        store_pack<GT, kVec, true>(row, (size_t)i * kParts + q, pack<GT, kVec>(f));
+            for (int e = 0; e < G; ++e) f[e] = sum[q * G + e];
+            store_pack<GT, true, true>(at, q, pack<GT, true>(f));
+        }
     }
 }
 
 // Blocks below part_blocks add the parts of cut runs; the others take one chunk of `each` table rows per group of threads,
 // whose runs are fetched together: most rows of a large vocabulary have none, and are only written.
-template <int DT, int GT, int kPacks, bool kVec>
+template <int DT, int GT, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
 {
-    constexpr int E = Pack<DT, kVec>::kElems;
+    constexpr int E = Elem<DT>::kElems;
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-    float acc[kPacks][E];
+    Two acc[kPacks][E / 2];
     if (blockIdx.x < a.part_blocks) {
         const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
         const unsigned part = unit / a.chunks, n = a.count[0], from = unit % a.chunks * a.group * kPacks + lane;
@@ -231,15 +254,17 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k)
 #pragma unroll
-                    for (int x = 0; x < E; ++x) acc[k][x] = 0.0f;
-                add_run<DT, kPacks, kVec>(acc, a, b > lo ? b : (unsigned)lo, e < hi ? e : hi, from);
+                    for (int x = 0; x < E / 2; ++x) acc[k][x] = all<Two>(0.0f);
+                add_run<DT, kPacks, kWhole>(acc, a, b > lo ? b : (unsigned)lo, e < hi ? e : hi, from, 0);
                 float* to = a.part + ((size_t)part * 2u + last) * a.part_stride;
 #pragma unroll
-                for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs) {
-                        if constexpr (E == 8)      store8(to + (size_t)(from + k * a.group) * 8u, acc[k]);
-                        else if constexpr (E == 4) *reinterpret_cast<float4*>(to + (size_t)(from + k * a.group) * 4u) = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
-                        else                       to[from + k * a.group] = acc[k][0];
+                for (int k = 0; k < kPacks; ++k)                     // a whole piece at the row's end too: part_stride is a multiple of eight
+                    if ((from + k * a.group) * E < a.hidden) {
+                        float f[E];
+#pragma unroll
+                        for (int x = 0; x < E; ++x) f[x] = x % 2 ? acc[k][x / 2].y : acc[k][x / 2].x;
+                        if constexpr (E == 8) store8(to + (size_t)(from + k * a.group) * 8u, f);
+                        else                  *reinterpret_cast<float4*>(to + (size_t)(from + k * a.group) * 4u) = make_float4(f[0], f[1], f[2], f[3]);
                     }
             }
         }
@@ -260,29 +285,33 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
             }
             const unsigned empty = __ballot_sync(0xFFFFFFFFu, mine && e == b), todo = __ballot_sync(0xFFFFFFFFu, mine && e != b && e - b <= kRunPart);
             // Rows without a token: one after the other, they are only stores, of consecutive vectors by consecutive lanes.
-            constexpr int G = Pack<GT, kVec>::kElems, kParts = E / G;
-            Pack<GT, kVec> zero;
-#pragma unroll
-            for (int w = 0; w < Pack<GT, kVec>::kWords; ++w) zero.w[w] = 0u;
+            constexpr int G = Elem<GT>::kElems, kParts = E / G;
+            const Pack<GT, true> zero = {};
             const unsigned zero_from = (from - lane) * kParts + lane;
             for (unsigned left = empty; left; left &= left - 1u) {
                 void* row = row_at(a.dtable, (size_t)first + __ffs(left) - 1, a.dtable_stride);
+                const int s = kWhole ? 0 : behind<GT, E>(row);
 #pragma unroll
-                for (int k = 0; k < kPacks * kParts; ++k)
-                    if (zero_from + k * a.group < a.packs * kParts) store_pack<GT, kVec, true>(row, zero_from + k * a.group, zero);
+                for (int k = 0; k < kPacks * kParts; ++k) {
+                    const int e0 = (int)((zero_from + k * a.group) * G) - s;
+                    if (touches<G>(e0, a.hidden)) store_piece<GT, kWhole, true>(row, a.hidden, e0, zero);
+                }
             }
             for (unsigned left = todo; left; left &= left - 1u) {
                 const int r = __ffs(left) - 1;
                 const unsigned row_v = __shfl_sync(0xFFFFFFFFu, v, r), row_b = __shfl_sync(0xFFFFFFFFu, b, r), row_e = __shfl_sync(0xFFFFFFFFu, e, r);
-#pragma unroll
-                for (int k = 0; k < kPacks; ++k)
-#pragma unroll
-                    for (int x = 0; x < E; ++x) acc[k][x] = 0.0f;
-                add_run<DT, kPacks, kVec>(acc, a, row_b, row_e, from);
                 void* row = row_at(a.dtable, row_v, a.dtable_stride);
+                const int s = kWhole ? 0 : behind<GT, E>(row);
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k)
-                    if (from + k * a.group < a.packs) put_gradient<GT, E>(a, row, from + k * a.group, acc[k]);
+#pragma unroll
+                    for (int x = 0; x < E / 2; ++x) acc[k][x] = all<Two>(0.0f);
+                add_run<DT, kPacks, kWhole>(acc, a, row_b, row_e, from, s);
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k) {
+                    const int e0 = (int)((from + k * a.group) * E) - s;
+                    if (touches<E>(e0, a.hidden)) put_gradient<GT, E, kWhole>(a, row, e0, acc[k]);
+                }
             }
         }
     }
@@ -312,10 +341,16 @@ __global__ void __launch_bounds__(256) k_embedding_join(const TableArgs a)
         sum[slice][lane] = s;
         __syncthreads();
         if (threadIdx.x < kJoinColumns && column + threadIdx.x < a.hidden) {
-            float f[1] = {0.0f};
+            float f[1] = {0.0f}, old[1];
 #pragma unroll
             for (int o = 0; o < 8; ++o) f[0] += reinterpret_cast<const float*>(sum[o])[threadIdx.x];
-            put_gradient<GT, 1>(a, row_at(a.dtable, v, a.dtable_stride), column + threadIdx.x, f);
+            f[0] *= a.scale;
+            void* row = row_at(a.dtable, v, a.dtable_stride);
+            if (a.accumulate) {
+                unpack<GT, false>(old, load_pack<GT, false>(row, column + threadIdx.x));
+                f[0] = __fadd_rn(old[0], f[0]);
+            }
+            store_pack<GT, false>(row, column + threadIdx.x, pack<GT, false>(f));
         }
         __syncthreads();
     }
@@ -328,10 +363,13 @@ struct RowShape {
     unsigned group, chunks;
 };
 
-// Threads (at most `most`) and chunks, of about the same length, for a row of `packs` packs, kPacks a thread.
-static RowShape row_shape(size_t packs, int per_thread, size_t most = 256)
+// Pieces of E elements that a row of `hidden` may be cut into.
+static size_t pieces(size_t hidden, int elems, bool whole) { return whole ? hidden / elems : (hidden + 2 * elems - 2) / elems; }
+
+// Threads (at most 256) and chunks, of about the same length, for a row of `packs` pieces, per_thread of them a thread.
+static RowShape row_shape(size_t packs, int per_thread)
 {
-    const size_t threads = (packs + per_thread - 1) / per_thread, chunks = (threads + most - 1) / most;
+    const size_t threads = (packs + per_thread - 1) / per_thread, chunks = (threads + 255) / 256;
     return {(unsigned)(((threads + chunks - 1) / chunks + 31) / 32 * 32), (unsigned)chunks};
 }
 
@@ -346,13 +384,13 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
     a.table_stride = (n.table_stride ? n.table_stride : n.hidden) * e;
     a.out_stride = (n.out_stride ? n.out_stride : n.hidden) * e;
     a.vocab_start = n.vocab_start, a.vocab_rows = (unsigned)n.vocab_rows, a.tokens = (unsigned)n.tokens;
-    a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
-    a.scale = n.scale;
+    a.hidden = (unsigned)n.hidden, a.scale = n.scale;
+    const size_t packs = pieces(n.hidden, 16 / (int)e, vec);
     const auto typed = [&](auto id, auto dt) {
         using Id = decltype(id);
         constexpr int DT = decltype(dt)::value;
         const auto run = [&](auto kernel, int tokens, int per_thread) {
-            const RowShape s = row_shape(a.packs, per_thread);
+            const RowShape s = row_shape(packs, per_thread);
             a.group = s.group, a.chunks = s.chunks;
             const unsigned long long units = (n.tokens + tokens - 1) / tokens * s.chunks;
             if (units > kMaxUnits) return (int)NUNA_ERR_TOO_LARGE;
@@ -360,9 +398,9 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
             const unsigned groups = 256u / s.group;
             return launch_op(kernel, Shape{(unsigned)((units + groups - 1) / groups), groups * s.group, 0, 1}, flags, stream, a);
         };
-        const bool few = (unsigned long long)n.tokens * a.packs <= 4ull * kSms * 512ull;     // too few for every SM to hold more than one a thread
+        const bool few = (unsigned long long)n.tokens * packs <= 4ull * kSms * 512ull;     // too few for every SM to hold more than one a thread
         if (vec) return few ? run(k_embedding_lookup<Id, DT, 1, 1, true>, 1, 1) : run(k_embedding_lookup<Id, DT, 4, 2, true>, 4, 2);
-        return few ? run(k_embedding_lookup<Id, DT, 1, 1, false>, 1, 1) : run(k_embedding_lookup<Id, DT, 2, 8, false>, 2, 8);
+        return few ? run(k_embedding_lookup<Id, DT, 1, 1, false>, 1, 1) : run(k_embedding_lookup<Id, DT, 4, 1, false>, 4, 1);
     };
     return with_dtype(n.dtype, [&](auto dt) { return n.id_bytes == 8 ? typed((long long)0, dt) : typed(0, dt); });
 }
@@ -399,14 +437,14 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     a.part = reinterpret_cast<float*>(words(w.part));
     a.dout_stride = (n.dout_stride ? n.dout_stride : n.hidden) * e;
     a.dtable_stride = (n.dtable_stride ? n.dtable_stride : n.hidden) * ge;
-    a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden), a.part_stride = (unsigned)part_stride(n.hidden), a.hidden = (unsigned)n.hidden;
+    a.part_stride = (unsigned)part_stride(n.hidden), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     a.scale = n.scale, a.accumulate = accumulate, a.whole_sectors = !(((uintptr_t)n.dtable | a.dtable_stride) & 31u);
     a.parts = n.tokens > kRunPart ? (unsigned)((n.tokens + kRunPart - 1) / kRunPart) : 0u;
     a.rows = (unsigned)(accumulate ? n.tokens : n.vocab_rows);
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const auto run = [&](auto rows, auto join, int per_thread) {
-            const RowShape sh = row_shape(a.packs, per_thread);
+            const RowShape sh = row_shape(pieces(n.hidden, Elem<DT>::kElems, vec), per_thread);
             a.group = sh.group, a.chunks = sh.chunks;
             const unsigned groups = 256u / sh.group;
             const auto blocks = [&](unsigned long long units) { return (units + groups - 1) / groups; };
@@ -427,7 +465,7 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
         const auto typed = [&](auto gt) {
             constexpr int GT = decltype(gt)::value;
             if (vec) return run(k_embedding_rows<DT, GT, 2, true>, k_embedding_join<GT>, 2);
-            return run(k_embedding_rows<DT, GT, 4, false>, k_embedding_join<GT>, 4);
+            return run(k_embedding_rows<DT, GT, 1, false>, k_embedding_join<GT>, 1);
         };
         return n.grad_dtype == NUNA_F32 ? typed(std::integral_constant<int, kF32>{}) : typed(dt);
     });

@@ -67,15 +67,16 @@ struct MoveArgs {
     float* dweights;
     size_t x_stride, src_stride, y_stride, out_stride;               // bytes
     unsigned units, token_blocks;                                    // tokens * chunks; the blocks behind those zero rows that no pair has
-    unsigned topk, rows, packs, chunks, group;                       // packs in a row, chunks of a row, threads of a chunk
+    unsigned tokens, topk, rows, hidden, packs, chunks, group;       // pieces in a row at most, chunks of a row, threads of a chunk
 };
 
 constexpr unsigned kZeroRows = 64;                                   // rows that a block looks at
 
 // Zeroes those of the block's kZeroRows expert rows that no pair has.
-template <int DT, bool kVec>
+template <int DT, bool kWhole>
 __device__ __forceinline__ void zero_empty_rows(const MoveArgs& a)
 {
+    constexpr int E = Elem<DT>::kElems;
     __shared__ unsigned empty[kZeroRows / 32u];
     const unsigned first = (blockIdx.x - a.token_blocks) * kZeroRows, r = first + threadIdx.x;
     if (threadIdx.x < kZeroRows) {
@@ -83,23 +84,26 @@ __device__ __forceinline__ void zero_empty_rows(const MoveArgs& a)
         if ((threadIdx.x & 31u) == 0u) empty[threadIdx.x / 32u] = votes;
     }
     __syncthreads();
-    Pack<DT, kVec> zero;
-#pragma unroll
-    for (int w = 0; w < Pack<DT, kVec>::kWords; ++w) zero.w[w] = 0u;
+    const Pack<DT, true> zero = {};
     for (unsigned q = 0; q < kZeroRows / 32u; ++q)
         for (unsigned left = empty[q]; left; left &= left - 1u) {
             void* row = row_at(a.out, (size_t)first + q * 32u + __ffs(left) - 1u, a.out_stride);
-            for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x) store_pack<DT, kVec, true>(row, i, zero);
+            const int s = kWhole ? 0 : behind<DT, E>(row);
+            for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x)
+                if (touches<E>((int)(i * E) - s, a.hidden)) store_piece<DT, kWhole, true>(row, a.hidden, (int)(i * E) - s, zero);
         }
 }
 
-template <int DT, int kPacks, bool kVec>
+// Every token's row to its pairs' rows.  Whole vectors are read once; rows that are cut otherwise are cut as each of the rows
+// that are written, and read again for each (from L1).
+template <int DT, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
 {
-    constexpr int kAhead = 8;                                        // rows of the map that are fetched together
+    constexpr int E = Elem<DT>::kElems;
+    constexpr int kAhead = kWhole ? 8 : 4;                           // rows of the map that are fetched together
     pdl_wait();
     if (blockIdx.x >= a.token_blocks) {
-        zero_empty_rows<DT, kVec>(a);
+        zero_empty_rows<DT, kWhole>(a);
     } else {
         const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
         const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
@@ -107,33 +111,55 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
             const size_t token = unit / a.chunks;
             const unsigned from = unit % a.chunks * a.group * kPacks + lane;
             const int* map = a.row_of_pair + token * a.topk;
-            Pack<DT, kVec> p[kPacks];
+            Piece<DT, kWhole> p[kWhole ? 1 : kAhead][kPacks];
+            Source source[kWhole ? 1 : kAhead];
+            if constexpr (kWhole) {
+                source[0] = source_of<DT, kWhole>(a.x, token, a.x_stride, a.tokens, a.hidden, 0);
 #pragma unroll
-            for (int k = 0; k < kPacks; ++k)
-                if (from + k * a.group < a.packs) p[k] = load_pack<DT, kVec>(row_at(a.x, token, a.x_stride), from + k * a.group);
+                for (int k = 0; k < kPacks; ++k)
+                    if (from + k * a.group < a.packs) fetch_piece<DT, kWhole>(p[0][k], source[0], from + k * a.group, 0, a.hidden);
+            }
             for (unsigned j0 = 0; j0 < a.topk; j0 += kAhead) {
                 unsigned row[kAhead];
+                int s[kAhead];
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j) row[j] = j0 + j < a.topk ? (unsigned)map[j0 + j] : 0xFFFFFFFFu;
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j) {
-                    if (row[j] >= a.rows) continue;
-                    void* out = row_at(a.out, row[j], a.out_stride);
+                    s[j] = 0;
+                    if constexpr (!kWhole) {
+                        if (row[j] < a.rows) {
+                            s[j] = behind<DT, E>(row_at(a.out, row[j], a.out_stride));
+                            source[j] = source_of<DT, kWhole>(a.x, token, a.x_stride, a.tokens, a.hidden, s[j]);
 #pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (from + k * a.group < a.packs) store_pack<DT, kVec, true>(out, from + k * a.group, p[k]);
+                            for (int k = 0; k < kPacks; ++k) {
+                                const int e0 = (int)((from + k * a.group) * E) - s[j];
+                                if (touches<E>(e0, a.hidden)) fetch_piece<DT, kWhole>(p[j][k], source[j], from + k * a.group, e0, a.hidden);
+                            }
+                        }
+                    }
                 }
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (row[j] < a.rows)
+#pragma unroll
+                        for (int k = 0; k < kPacks; ++k) {
+                            const int e0 = (int)((from + k * a.group) * E) - s[j];
+                            if (touches<E>(e0, a.hidden))
+                                store_piece<DT, kWhole, true>(row_at(a.out, row[j], a.out_stride), a.hidden, e0,
+                                                              settle_piece<DT, kWhole>(p[kWhole ? 0 : j][k], source[kWhole ? 0 : j]));
+                        }
             }
         }
     }
     pdl_trigger();
 }
 
-template <int DT, int kPacks, bool kVec>
+template <int DT, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
 {
-    constexpr int E = Pack<DT, kVec>::kElems;
-    constexpr int kAhead = kVec && kPacks == 2 ? 4 : 8;              // expert rows in flight
+    constexpr int E = Elem<DT>::kElems;
+    constexpr int kAhead = kWhole && kPacks == 1 ? 8 : 4;            // expert rows in flight
     pdl_wait();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
@@ -142,56 +168,64 @@ __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
         const unsigned from = unit % a.chunks * a.group * kPacks + lane;
         const int* map = a.row_of_pair + token * a.topk;
         const float* weights = a.weights ? a.weights + token * a.topk : nullptr;
-        float acc[kPacks][E];
+        void* y = row_at(a.y, token, a.y_stride);
+        const int s = kWhole ? 0 : behind<DT, E>(y);
+        Two acc[kPacks][E / 2];
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[k][e] = 0.0f;
+            for (int e = 0; e < E / 2; ++e) acc[k][e] = all<Two>(0.0f);
         for (unsigned j0 = 0; j0 < a.topk; j0 += kAhead) {
             unsigned row[kAhead];
             float w[kAhead];
-            Pack<DT, kVec> v[kAhead][kPacks];
+            Piece<DT, kWhole> v[kAhead][kPacks];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 row[j] = j0 + j < a.topk ? (unsigned)map[j0 + j] : 0xFFFFFFFFu;
                 w[j] = weights && j0 + j < a.topk ? weights[j0 + j] : 1.0f;
             }
+            Source source[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (row[j] < a.rows) {
+                    source[j] = source_of<DT, kWhole>(a.src, row[j], a.src_stride, a.rows, a.hidden, s);
+#pragma unroll
+                    for (int k = 0; k < kPacks; ++k) {
+                        const int e0 = (int)((from + k * a.group) * E) - s;
+                        if (touches<E>(e0, a.hidden)) fetch_piece<DT, kWhole>(v[j][k], source[j], from + k * a.group, e0, a.hidden);
+                    }
+                }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
                 if (row[j] < a.rows)
 #pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (from + k * a.group < a.packs) v[j][k] = load_pack<DT, kVec>(row_at(a.src, row[j], a.src_stride), from + k * a.group);
+                    for (int k = 0; k < kPacks; ++k) {
+                        Two f[E / 2];
+                        unpack<DT, true>(f, settle_piece<DT, kWhole>(v[j][k], source[j]));
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-                if (row[j] < a.rows)
-#pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (from + k * a.group < a.packs) {
-                            float f[E];
-                            unpack<DT, kVec>(f, v[j][k]);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) acc[k][e] = fmaf(w[j], f[e], acc[k][e]);
-                        }
+                        for (int e = 0; e < E / 2; ++e) acc[k][e] = mad(all<Two>(w[j]), f[e], acc[k][e]);
+                    }
         }
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k)
-            if (from + k * a.group < a.packs) store_pack<DT, kVec>(row_at(a.y, token, a.y_stride), from + k * a.group, pack<DT, kVec>(acc[k]));
+        for (int k = 0; k < kPacks; ++k) {
+            const int e0 = (int)((from + k * a.group) * E) - s;
+            if (touches<E>(e0, a.hidden)) store_piece<DT, kWhole>(y, a.hidden, e0, pack<DT, true>(acc[k]));
+        }
     }
     pdl_trigger();
 }
 
-// A token per group of threads, which goes over the row kPacks packs a thread at a time; kBatch pairs' products are summed
+// A token per group of threads, which goes over the row kPacks pieces a thread at a time; kBatch pairs' products are summed
 // together, and over the group at the end of the row.
-template <int DT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(512) k_expert_combine_backward(const MoveArgs a)
+template <int DT, int kPacks, bool kWhole>
+__global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs a)
 {
-    constexpr int E = Pack<DT, kVec>::kElems;
-    constexpr int kBatch = 4;
-    __shared__ float red[2][16][kBatch];
+    constexpr int E = Elem<DT>::kElems;
+    constexpr int kBatch = kWhole ? 4 : 2;                           // pairs in flight
+    __shared__ float red[2][8][kBatch];
     pdl_wait();
     if (blockIdx.x >= a.token_blocks) {
-        zero_empty_rows<DT, kVec>(a);
+        zero_empty_rows<DT, kWhole>(a);
     } else {
         const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group, warps = a.group / 32u;
         const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
@@ -200,55 +234,79 @@ __global__ void __launch_bounds__(512) k_expert_combine_backward(const MoveArgs 
         unsigned turn = 0;
         for (unsigned j0 = 0; j0 < a.topk; j0 += kBatch, turn ^= 1u) {
             unsigned row[kBatch];
-            float w[kBatch], dot[kBatch];
+            float w[kBatch];
+            int s[kBatch];
+            Two dot[kBatch];
+            Source src[kBatch], x[kWhole ? 1 : kBatch];              // whole vectors of dy serve all rows; otherwise each row has them cut as itself
+            if constexpr (kWhole) x[0] = source_of<DT, kWhole>(a.x, token, a.x_stride, a.tokens, a.hidden, 0);
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 const bool is = live && j0 + j < a.topk;
                 row[j] = is ? (unsigned)a.row_of_pair[token * a.topk + j0 + j] : 0xFFFFFFFFu;
                 w[j] = is ? a.weights[token * a.topk + j0 + j] : 0.0f;
-                dot[j] = 0.0f;
+                dot[j] = all<Two>(0.0f);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                s[j] = kWhole || row[j] >= a.rows ? 0 : behind<DT, E>(row_at(a.out, row[j], a.out_stride));
+                src[j] = source_of<DT, kWhole>(a.src, row[j], a.src_stride, a.rows, a.hidden, s[j]);
+                if constexpr (!kWhole) x[j] = source_of<DT, kWhole>(a.x, token, a.x_stride, a.tokens, a.hidden, s[j]);
             }
             for (unsigned base = lane; base < a.packs; base += a.group * kPacks) {
-                Pack<DT, kVec> dy[kPacks], v[kBatch][kPacks];
-                if (live)
+                Piece<DT, kWhole> dy[kWhole ? 1 : kBatch][kPacks], v[kBatch][kPacks];
+                if constexpr (kWhole) {
+                    if (live) {
 #pragma unroll
-                    for (int k = 0; k < kPacks; ++k)
-                        if (base + k * a.group < a.packs) dy[k] = load_pack<DT, kVec>(row_at(a.x, token, a.x_stride), base + k * a.group);
-                if (a.dweights)
+                        for (int k = 0; k < kPacks; ++k)
+                            if (base + k * a.group < a.packs) fetch_piece<DT, kWhole>(dy[0][k], x[0], base + k * a.group, 0, a.hidden);
+                    }
+                }
 #pragma unroll
-                    for (int j = 0; j < kBatch; ++j)
-                        if (row[j] < a.rows)
+                for (int j = 0; j < kBatch; ++j)
+                    if (row[j] < a.rows)
 #pragma unroll
-                            for (int k = 0; k < kPacks; ++k)
-                                if (base + k * a.group < a.packs)
-                                    v[j][k] = load_pack<DT, kVec>(row_at(a.src, row[j], a.src_stride), base + k * a.group);
+                        for (int k = 0; k < kPacks; ++k) {
+                            const int e0 = (int)((base + k * a.group) * E) - s[j];
+                            if (touches<E>(e0, a.hidden)) {
+                                if constexpr (!kWhole) fetch_piece<DT, kWhole>(dy[j][k], x[j], base + k * a.group, e0, a.hidden);
+                                if (a.dweights) fetch_piece<DT, kWhole>(v[j][k], src[j], base + k * a.group, e0, a.hidden);
+                            }
+                        }
 #pragma unroll
-                for (int k = 0; k < kPacks; ++k)
-                    if (live && base + k * a.group < a.packs) {
-                        float g[E];
-                        unpack<DT, kVec>(g, dy[k]);
+                for (int j = 0; j < kBatch; ++j)
+                    if (row[j] < a.rows)
 #pragma unroll
-                        for (int j = 0; j < kBatch; ++j)
-                            if (row[j] < a.rows) {
-                                float f[E];
+                        for (int k = 0; k < kPacks; ++k) {
+                            const int e0 = (int)((base + k * a.group) * E) - s[j];
+                            if (touches<E>(e0, a.hidden)) {
+                                Two g[E / 2], f[E / 2];
+                                unpack<DT, true>(g, settle_piece<DT, kWhole>(dy[kWhole ? 0 : j][k], x[kWhole ? 0 : j]));
                                 if (a.dweights) {
-                                    unpack<DT, kVec>(f, v[j][k]);
+                                    unpack<DT, true>(f, settle_piece<DT, kWhole>(v[j][k], src[j]));
+                                    if (!kWhole && !inside<E>(e0, a.hidden)) {
 #pragma unroll
-                                    for (int e = 0; e < E; ++e) dot[j] = fmaf(g[e], f[e], dot[j]);
+                                        for (int e = 0; e < E; ++e)
+                                            if (e0 + e < 0 || e0 + e >= (int)a.hidden) half(f[e / 2], e) = half(g[e / 2], e) = 0.0f;
+                                    }
+#pragma unroll
+                                    for (int e = 0; e < E / 2; ++e) dot[j] = mad(g[e], f[e], dot[j]);
                                 }
 #pragma unroll
-                                for (int e = 0; e < E; ++e) f[e] = w[j] * g[e];
-                                store_pack<DT, kVec, true>(row_at(a.out, row[j], a.out_stride), base + k * a.group, pack<DT, kVec>(f));
+                                for (int e = 0; e < E / 2; ++e) f[e] = all<Two>(w[j]) * g[e];
+                                store_piece<DT, kWhole, true>(row_at(a.out, row[j], a.out_stride), a.hidden, e0, pack<DT, true>(f));
                             }
-                    }
+                        }
             }
             if (a.dweights) {
-                warp_sum<kBatch>(dot);
+                float sum[kBatch];
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) sum[j] = total(dot[j]);
+                warp_sum<kBatch>(sum);
                 if (warps > 1u) {
                     const unsigned warp = threadIdx.x >> 5;
                     if ((threadIdx.x & 31u) == 0u)
 #pragma unroll
-                        for (int j = 0; j < kBatch; ++j) red[turn][warp][j] = dot[j];
+                        for (int j = 0; j < kBatch; ++j) red[turn][warp][j] = sum[j];
                     __syncthreads();                                 // the next batch has the other half of `red`
                     if (lane < kBatch) {
                         float s = 0.0f;
@@ -258,7 +316,7 @@ __global__ void __launch_bounds__(512) k_expert_combine_backward(const MoveArgs 
                 } else if (live && lane == 0u) {
 #pragma unroll
                     for (int j = 0; j < kBatch; ++j)
-                        if (j0 + j < a.topk) a.dweights[token * a.topk + j0 + j] = dot[j];
+                        if (j0 + j < a.topk) a.dweights[token * a.topk + j0 + j] = sum[j];
                 }
             }
         }
@@ -270,7 +328,10 @@ __global__ void __launch_bounds__(512) k_expert_combine_backward(const MoveArgs 
 
 static size_t stride_bytes(size_t stride, size_t hidden, int dtype) { return (stride ? stride : hidden) * dtype_bytes(dtype); }
 
-// Launches a row mover with kPacks packs a thread in groups of at most `most` threads, which take chunks of a row, or (`whole`)
+// Pieces of 16 bytes that a row may be cut into.
+static unsigned pieces(size_t hidden, size_t size, bool whole) { return (unsigned)(whole ? hidden * size / 16 : (hidden + 2 * (16 / size) - 2) / (16 / size)); }
+
+// Launches a row mover with kPacks pieces a thread in groups of at most `most` threads, which take chunks of a row, or (`whole`)
 // a row in several steps.
 template <typename Kernel>
 static int move_rows(Kernel kernel, MoveArgs& a, size_t tokens, int per_thread, unsigned most, bool whole, unsigned flags, void* stream)
@@ -296,15 +357,16 @@ static int dispatch(const nuna_expert_dispatch_t& n, unsigned flags, void* strea
     MoveArgs a = {};
     a.x = n.x, a.row_of_pair = n.row_of_pair, a.pair_of_row = n.pair_of_row, a.out = n.out;
     a.x_stride = stride_bytes(n.x_stride, n.hidden, n.dtype), a.out_stride = stride_bytes(n.out_stride, n.hidden, n.dtype);
-    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
+    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = pieces(n.hidden, e, vec), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     const size_t tokens = n.topk ? n.tokens : 0;
     if (vec) {                                                       // bits are copied: a vector is a vector
+        a.hidden = (unsigned)(n.hidden * e / 4);
         return (unsigned long long)tokens * a.packs <= 4ull * kSms * 512ull
                    ? move_rows(k_expert_dispatch<kF32, 1, true>, a, tokens, 1, 256, false, flags, stream)
                    : move_rows(k_expert_dispatch<kF32, 4, true>, a, tokens, 4, 256, false, flags, stream);
     }
-    if (n.dtype == NUNA_F32) return move_rows(k_expert_dispatch<kF32, 4, false>, a, tokens, 4, 256, false, flags, stream);
-    return move_rows(k_expert_dispatch<kBf16, 4, false>, a, tokens, 4, 256, false, flags, stream);
+    if (n.dtype == NUNA_F32) return move_rows(k_expert_dispatch<kF32, 1, false>, a, tokens, 1, 256, false, flags, stream);
+    return move_rows(k_expert_dispatch<kBf16, 1, false>, a, tokens, 1, 256, false, flags, stream);
 }
 
 static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
@@ -314,10 +376,10 @@ static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
     MoveArgs a = {};
     a.src = n.src, a.row_of_pair = n.row_of_pair, a.weights = n.weights, a.y = n.y;
     a.src_stride = stride_bytes(n.src_stride, n.hidden, n.dtype), a.y_stride = stride_bytes(n.y_stride, n.hidden, n.dtype);
-    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
+    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = pieces(n.hidden, e, vec), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine<DT, 4, false>, a, n.tokens, 4, 256, false, flags, stream);
+        if (!vec) return move_rows(k_expert_combine<DT, 1, false>, a, n.tokens, 1, 256, false, flags, stream);
         return (unsigned long long)n.tokens * a.packs <= 2ull * kSms * 512ull
                    ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, 256, false, flags, stream)
                    : move_rows(k_expert_combine<DT, 2, true>, a, n.tokens, 2, 256, false, flags, stream);
@@ -334,11 +396,11 @@ static int combine_backward(const nuna_expert_combine_grad_t& n, unsigned flags,
     a.out = n.dsrc, a.dweights = n.dweights;
     a.x_stride = stride_bytes(n.dy_stride, n.hidden, n.dtype), a.src_stride = stride_bytes(n.src_stride, n.hidden, n.dtype);
     a.out_stride = stride_bytes(n.dsrc_stride, n.hidden, n.dtype);
-    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = (unsigned)(vec ? n.hidden * e / 16 : n.hidden);
+    a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = pieces(n.hidden, e, vec), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     const size_t tokens = n.topk ? n.tokens : 0;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine_backward<DT, 4, false>, a, tokens, 4, 512, true, flags, stream);
+        if (!vec) return move_rows(k_expert_combine_backward<DT, 1, false>, a, tokens, 1, 256, true, flags, stream);
         return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, 256, true, flags, stream);
     });
 }

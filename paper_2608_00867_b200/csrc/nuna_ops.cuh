@@ -259,6 +259,117 @@ __device__ __forceinline__ void* row_at(void* base, size_t row, size_t stride_by
     return reinterpret_cast<void*>(reinterpret_cast<uintptr_t>(base) + row * stride_bytes);
 }
 
+// ---- pieces of rows that are not whole vectors ---------------------------------------------------------
+//
+// Where rows are not whole 16-byte vectors at 16-byte addresses (odd lengths, odd strides), a row that is written is cut at its
+// own 16-byte boundaries: piece i is the E elements from E * i - s on, s being how far behind a boundary the row begins.  All
+// pieces but the first and the last are then stored as vectors.  A row that is read lies at some other distance from a boundary,
+// the same for all of its pieces: a piece is shifted out of the two vectors around it, 2 loads and 4 shifts instead of E loads
+// (lookup of 20011 rows of 1037 f16: 26.5 -> 20 us).  Those two vectors may reach up to 14 bytes beyond the row, into its
+// neighbours or the gaps; what comes from there is not used, and the first and the last row of a matrix, where nothing need be
+// there, are read element by element.
+template <int DT, bool kWhole> struct Piece {
+    uint32_t w[kWhole ? 4 : 8];
+};
+
+// Elements from which a row at this address is behind a boundary of E of its elements.
+template <int DT, int E>
+__device__ __forceinline__ int behind(const void* row) { return (int)(((uintptr_t)row & (E * Elem<DT>::kBytes - 1u)) / Elem<DT>::kBytes); }
+
+// A row that is read in the pieces of a row that begins s elements behind a boundary: piece i is shifted by m bytes out of the
+// vectors at at + 16 * i and behind it.
+struct Source {
+    const char* at;
+    unsigned m;
+    bool by_element;
+};
+
+template <int DT, bool kWhole>
+__device__ __forceinline__ Source source_of(const void* base, size_t row, size_t stride, size_t rows, unsigned hidden, int s)
+{
+    const char* from = static_cast<const char*>(row_at(base, row, stride)) - s * Elem<DT>::kBytes;
+    if constexpr (kWhole) return {from, 0u, false};
+    if (row == 0 || row + 1 == rows || hidden < (unsigned)Elem<DT>::kElems) return {from, 0u, true};
+    const unsigned m = (unsigned)(uintptr_t)from & 15u;
+    return {from - m, m, false};
+}
+
+// Starts loading piece i, which begins at element e0 = E * i - s; what is outside of the row is not defined.  At least one of
+// its elements is inside.
+template <int DT, bool kWhole>
+__device__ __forceinline__ void fetch_piece(Piece<DT, kWhole>& p, const Source& src, unsigned i, int e0, unsigned hidden)
+{
+    constexpr int kBytes = Elem<DT>::kBytes, E = Elem<DT>::kElems;
+    const char* at = src.at + (size_t)i * 16u;
+    if constexpr (kWhole) {
+        const uint4 v = ld_src(reinterpret_cast<const uint4*>(at));
+        p.w[0] = v.x, p.w[1] = v.y, p.w[2] = v.z, p.w[3] = v.w;
+    } else if (src.by_element) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) p.w[k] = 0u;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e0 + e >= 0 && e0 + e < (int)hidden) {
+                if constexpr (DT == kF32) p.w[e] = ld_src32(reinterpret_cast<const uint32_t*>(at) + e);
+                else                      p.w[e / 2] |= (uint32_t)ld_src16(reinterpret_cast<const uint16_t*>(at) + e) << (16 * (e % 2));
+            }
+    } else {
+        // the first vector holds elements e0 - m / kBytes ... + E-1 of the row, the second the E behind them: loaded if one is in the row
+        const int left = e0 + E - (int)(src.m / kBytes);
+        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.gt.s32 p, %9, 0;\n\tsetp.lt.s32 q, %9, %10;\n\tsetp.ne.and.u32 q, %11, 0, q;\n\t"
+                     "@p ld.global.v4.u32 {%0,%1,%2,%3}, [%8];\n\t@q ld.global.v4.u32 {%4,%5,%6,%7}, [%8+16];\n\t}"
+                     : "=r"(p.w[0]), "=r"(p.w[1]), "=r"(p.w[2]), "=r"(p.w[3]), "=r"(p.w[4]), "=r"(p.w[5]), "=r"(p.w[6]), "=r"(p.w[7])
+                     : "l"(at), "r"(left), "r"((int)hidden), "r"(src.m));
+    }
+}
+
+// The elements of a piece that has arrived.
+template <int DT, bool kWhole>
+__device__ __forceinline__ Pack<DT, true> settle_piece(const Piece<DT, kWhole>& p, const Source& src)
+{
+    Pack<DT, true> v;
+    if constexpr (kWhole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = p.w[i];
+    } else {
+        // two words, one word, part of a word
+        uint32_t t[6], u[5];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) t[i] = src.m & 8u ? p.w[i + 2] : p.w[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) u[i] = src.m & 4u ? t[i + 1] : t[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.w[i] = DT == kF32 ? u[i] : __funnelshift_r(u[i], u[i + 1], src.m * 8u);    // modulo 32
+    }
+    return v;
+}
+
+// Whether a piece is wholly inside its row.
+template <int E>
+__device__ __forceinline__ bool inside(int e0, unsigned hidden) { return e0 >= 0 && (unsigned)e0 + E <= hidden; }
+
+// Whether a piece has an element of its row.
+template <int E>
+__device__ __forceinline__ bool touches(int e0, unsigned hidden) { return e0 > -E && e0 < (int)hidden; }
+
+// Stores those elements of a piece that are in the row; row + e0 is at a 16-byte boundary.
+template <int DT, bool kWhole, bool kStream = false>
+__device__ __forceinline__ void store_piece(void* row, unsigned hidden, int e0, const Pack<DT, true>& v)
+{
+    constexpr int kBytes = Elem<DT>::kBytes, E = Elem<DT>::kElems;
+    char* at = static_cast<char*>(row) + (long long)e0 * kBytes;
+    if (kWhole || inside<E>(e0, hidden)) {
+        store_pack<DT, true, kStream>(at, 0, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e0 + e >= 0 && e0 + e < (int)hidden) {
+                if constexpr (DT == kF32) reinterpret_cast<uint32_t*>(at)[e] = v.w[e];
+                else                      reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(v.w[e / 2] >> (16 * (e % 2)));
+            }
+    }
+}
+
 // Pairs of binary32 in one instruction (sm_100's f32x2 forms: each half rounds as the plain instruction does).  The
 // element-wise loops of the norm are bound by instruction issue as much as by memory, and these halve their arithmetic.
 struct Two {

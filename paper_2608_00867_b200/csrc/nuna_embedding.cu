@@ -425,7 +425,7 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
         const Shape sort = sort_shape(n.tokens, 1u << s.bits);
         constexpr int kMost = sort_smem(kSortMaxWarps, 1024);
         const bool wide = n.id_bytes == 8;
-        int st = sort.smem <= 32 * 1024 ? NUNA_OK : wide ? allow_smem<k_embedding_sort<long long>>(kMost) : allow_smem<k_embedding_sort<int>>(kMost);
+        int st = wide ? allow_sort<k_embedding_sort<long long>>(sort, kMost) : allow_sort<k_embedding_sort<int>>(sort, kMost);
         if (st != NUNA_OK) return st;
         if ((st = launch_op(wide ? k_embedding_sort<long long> : k_embedding_sort<int>, sort, flags, stream, s)) != NUNA_OK) return st;
     }

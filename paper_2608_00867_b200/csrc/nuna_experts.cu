@@ -426,7 +426,7 @@ int nuna_expert_sort(const nuna_expert_sort_t* args, unsigned flags, void* strea
     s.smem += k.num_experts * 4u;
     constexpr int kMost = sort_smem(kSortMaxWarps, NUNA_MAX_EXPERTS) + NUNA_MAX_EXPERTS * 4;
     const bool wide = a.id_bytes == 8;
-    const int ok = s.smem <= 32 * 1024 ? NUNA_OK : wide ? allow_smem<k_expert_sort<long long>>(kMost) : allow_smem<k_expert_sort<int>>(kMost);
+    const int ok = wide ? allow_sort<k_expert_sort<long long>>(s, kMost) : allow_sort<k_expert_sort<int>>(s, kMost);
     if (ok != NUNA_OK) return ok;
     return launch_op(wide ? k_expert_sort<long long> : k_expert_sort<int>, s, effective_flags(flags, stream), stream, k);
 }

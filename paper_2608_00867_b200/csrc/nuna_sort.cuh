@@ -5,7 +5,7 @@
 // warps are summed bin by bin, every block reads the other blocks' totals out of their shared memory, and an item's place is
 //   items of smaller digits + those of its digit in earlier blocks, in earlier warps, earlier in its warp.
 // Nothing is decided by the order in which blocks run, there are no atomics, and the only waits are cluster barriers.  One
-// cluster of at most 8 blocks sorts all sizes: the rows that are moved by the result take far longer beyond some 10^5 items.
+// cluster of at most 16 blocks sorts all sizes: the rows that are moved by the result take far longer beyond some 10^5 items.
 #pragma once
 #include "nuna_ops.cuh"
 
@@ -13,7 +13,7 @@ namespace nuna {
 
 constexpr int kSortItems = 8;                            // items of a lane that are fetched together
 constexpr unsigned kSortMaxWarps = 32;
-constexpr unsigned kSortMaxCluster = 8;
+constexpr unsigned kSortMaxCluster = 16;                 // beyond 8 blocks a kernel has to ask for it (allow_sort)
 constexpr unsigned kNoDigit = 0xFFFFFFFFu;
 
 constexpr unsigned kSortSegments = 8;                    // cuts of a bin's counts by warp
@@ -198,16 +198,35 @@ __device__ __forceinline__ unsigned sort_pass(unsigned n, unsigned bins, unsigne
     return carry;
 }
 
-// Blocks of the cluster and warps of a block that sort n items.  One block takes up to kSortAlone: beyond, eight of them are
-// ahead of what their barriers cost.
-constexpr size_t kSortAlone = 4096;
-constexpr size_t kSortEach = 4;                          // items of a lane for which another warp is not worth its part in the sums
+// Blocks of the cluster and warps of a block that sort n items: one block, eight or sixteen, where what the warps save is more
+// than the cluster's barriers and the reads of its totals cost (by 128 experts: 1024 pairs 4.7 us in one block, 2048 6.4 | 4.6 in one
+// and in eight, 8192 5.8 | 5.6 in eight and in sixteen, 16384 7.9 | 6.0, 65536 18.5 | 12.4).  A warp takes four items a lane
+// before there is another one (2 | 4 | 8: 16384 pairs 9.0 | 8.0 | 7.6, 8192 tokens by 32768 rows 21.1 | 21.3 | 26.2 the whole gradient).
+constexpr size_t kSortAlone = 1024, kSortWide = 8192;
+constexpr size_t kSortEach = 4;
 inline Shape sort_shape(size_t n, unsigned bins)
 {
-    const unsigned cluster = n <= kSortAlone ? 1u : kSortMaxCluster;
+    const unsigned cluster = n <= kSortAlone ? 1u : n <= kSortWide ? 8u : kSortMaxCluster;
     const size_t warps = (n / cluster + 32 * kSortEach - 1) / (32 * kSortEach);
     const unsigned per_block = (unsigned)(warps < 4 ? 4 : warps > kSortMaxWarps ? kSortMaxWarps : warps);
     return Shape{cluster, per_block * 32u, sort_smem(per_block, bins), cluster};
+}
+
+// Lets a kernel have `bytes` of shared memory in clusters of up to kSortMaxCluster blocks.
+template <auto kKernel>
+int allow_sort(const Shape& s, int bytes)
+{
+    if (s.cluster <= 8u && s.smem <= 32 * 1024) return NUNA_OK;
+    static std::atomic<bool> done[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return NUNA_ERR_CUDA;
+    if (!done[dev].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess ||
+            cudaFuncSetAttribute(kKernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+            return NUNA_ERR_CUDA;
+        done[dev].store(true, std::memory_order_relaxed);
+    }
+    return NUNA_OK;
 }
 
 }  // namespace nuna

@@ -66,32 +66,38 @@ struct MoveArgs {
     void *y, *out;                                                   // token rows (written), expert rows (written)
     float* dweights;
     size_t x_stride, src_stride, y_stride, out_stride;               // bytes
-    unsigned units, token_blocks;                                    // tokens * chunks; the blocks behind those zero rows that no pair has
+    unsigned units, zero_blocks;                                     // tokens * chunks; blocks that zero rows that no pair has
     unsigned tokens, topk, rows, hidden, packs, chunks, group;       // pieces in a row at most, chunks of a row, threads of a chunk
 };
 
-constexpr unsigned kZeroRows = 64;                                   // rows that a block looks at
+constexpr unsigned kZeroRows = 32;                                   // rows that a block looks at
 
-// Zeroes those of the block's kZeroRows expert rows that no pair has.
+// Zeroes those of the block's kZeroRows expert rows that no pair has.  These blocks come first: one that has to write all of
+// its rows would otherwise be what the kernel ends with.
 template <int DT, bool kWhole>
 __device__ __forceinline__ void zero_empty_rows(const MoveArgs& a)
 {
     constexpr int E = Elem<DT>::kElems;
-    __shared__ unsigned empty[kZeroRows / 32u];
-    const unsigned first = (blockIdx.x - a.token_blocks) * kZeroRows, r = first + threadIdx.x;
-    if (threadIdx.x < kZeroRows) {
-        const unsigned votes = __ballot_sync(0xFFFFFFFFu, r < a.rows && a.pair_of_row[r] < 0);
-        if ((threadIdx.x & 31u) == 0u) empty[threadIdx.x / 32u] = votes;
-    }
-    __syncthreads();
+    const unsigned first = blockIdx.x * kZeroRows, lane = threadIdx.x & 31u;
+    const unsigned empty = __ballot_sync(0xFFFFFFFFu, first + lane < a.rows && a.pair_of_row[first + lane] < 0);        // every warp for itself
     const Pack<DT, true> zero = {};
-    for (unsigned q = 0; q < kZeroRows / 32u; ++q)
-        for (unsigned left = empty[q]; left; left &= left - 1u) {
-            void* row = row_at(a.out, (size_t)first + q * 32u + __ffs(left) - 1u, a.out_stride);
-            const int s = kWhole ? 0 : behind<DT, E>(row);
-            for (unsigned i = threadIdx.x; i < a.packs; i += blockDim.x)
-                if (touches<E>((int)(i * E) - s, a.hidden)) store_piece<DT, kWhole, true>(row, a.hidden, (int)(i * E) - s, zero);
+    for (unsigned left = empty; left; left &= left - 1u) {
+        char* row = static_cast<char*>(row_at(a.out, (size_t)first + __ffs(left) - 1u, a.out_stride));
+        const unsigned s = kWhole ? 0u : (unsigned)behind<DT, E>(row);
+        if constexpr (!kWhole) {                                     // what is in front of the first boundary and behind the last
+            const unsigned head = s ? E - s : 0u, tail = (a.hidden + s) / E * E - s, i = threadIdx.x;
+            if (a.hidden < 2u * E) {
+                if (i < a.hidden) store_pack<DT, false>(row, i, {0u});
+                continue;
+            }
+            if (i < head) store_pack<DT, false>(row, i, {0u});
+            if (tail + i < a.hidden) store_pack<DT, false>(row, tail + i, {0u});
         }
+        const unsigned from = s ? 1u : 0u, to = (a.hidden + s) / E;
+        row -= s * Elem<DT>::kBytes;
+#pragma unroll 4
+        for (unsigned i = from + threadIdx.x; i < to; i += blockDim.x) store_pack<DT, true, true>(row, i, zero);
+    }
 }
 
 // Every token's row to its pairs' rows.  Whole vectors are read once; rows that are cut otherwise are cut as each of the rows
@@ -102,11 +108,11 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
     constexpr int E = Elem<DT>::kElems;
     constexpr int kAhead = kWhole ? 8 : 4;                           // rows of the map that are fetched together
     pdl_wait();
-    if (blockIdx.x >= a.token_blocks) {
+    if (blockIdx.x < a.zero_blocks) {
         zero_empty_rows<DT, kWhole>(a);
     } else {
         const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
-        const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+        const unsigned unit = (blockIdx.x - a.zero_blocks) * groups + threadIdx.x / a.group;
         if (unit < a.units) {
             const size_t token = unit / a.chunks;
             const unsigned from = unit % a.chunks * a.group * kPacks + lane;
@@ -224,11 +230,11 @@ __global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs 
     constexpr int kBatch = kWhole ? 4 : 2;                           // pairs in flight
     __shared__ float red[2][8][kBatch];
     pdl_wait();
-    if (blockIdx.x >= a.token_blocks) {
+    if (blockIdx.x < a.zero_blocks) {
         zero_empty_rows<DT, kWhole>(a);
     } else {
         const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group, warps = a.group / 32u;
-        const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
+        const unsigned unit = (blockIdx.x - a.zero_blocks) * groups + threadIdx.x / a.group;
         const size_t token = unit;
         const bool live = unit < a.units;
         unsigned turn = 0;
@@ -343,11 +349,11 @@ static int move_rows(Kernel kernel, MoveArgs& a, size_t tokens, int per_thread, 
     const unsigned long long units = (unsigned long long)tokens * a.chunks;
     if (units > 0xFFFFFF00ull) return NUNA_ERR_TOO_LARGE;            // 32 bits count the units
     a.units = (unsigned)units;
-    a.token_blocks = (unsigned)((units + groups - 1) / groups);
-    const unsigned long long grid = a.token_blocks + (a.pair_of_row ? (a.rows + kZeroRows - 1ull) / kZeroRows : 0ull);
+    a.zero_blocks = a.pair_of_row ? (unsigned)((a.rows + kZeroRows - 1ull) / kZeroRows) : 0u;
+    const unsigned long long grid = a.zero_blocks + (units + groups - 1) / groups;
     if (grid > kMaxExtent) return NUNA_ERR_TOO_LARGE;
     if (grid == 0) return NUNA_OK;
-    return launch_op(kernel, Shape{(unsigned)grid, std::max(kZeroRows, groups * a.group), 0, 1}, flags, stream, a);
+    return launch_op(kernel, Shape{(unsigned)grid, groups * a.group, 0, 1}, flags, stream, a);
 }
 
 static int dispatch(const nuna_expert_dispatch_t& n, unsigned flags, void* stream)
@@ -379,7 +385,7 @@ static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
     a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = pieces(n.hidden, e, vec), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine<DT, 1, false>, a, n.tokens, 1, 256, false, flags, stream);
+        if (!vec) return move_rows(k_expert_combine<DT, 2, false>, a, n.tokens, 2, 256, false, flags, stream);
         return (unsigned long long)n.tokens * a.packs <= 2ull * kSms * 512ull
                    ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, 256, false, flags, stream)
                    : move_rows(k_expert_combine<DT, 2, true>, a, n.tokens, 2, 256, false, flags, stream);
@@ -401,7 +407,7 @@ static int combine_backward(const nuna_expert_combine_grad_t& n, unsigned flags,
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (!vec) return move_rows(k_expert_combine_backward<DT, 1, false>, a, tokens, 1, 256, true, flags, stream);
-        return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, 256, true, flags, stream);
+        return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, 128, true, flags, stream);
     });
 }
 

@@ -24,10 +24,10 @@ struct LookupArgs {
 // One chunk of kTokens tokens' rows per group of threads, kPacks pieces a thread and token: the tokens' ids are fetched together,
 // and then all of their pieces.
 template <typename Id, int DT, int kTokens, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_embedding_lookup(const LookupArgs a)
+__global__ void __launch_bounds__(256) k_embedding_lookup(const Padded<LookupArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
-    pdl_wait();
+    pdl_begin();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
     if (unit < a.units) {
@@ -95,10 +95,10 @@ struct SortArgs {
 // items[passes & 1 ^ 1]: the tokens with a row in the slice, by row and then by token; begin / end: each row's run; count: how
 // many tokens that is, and how many runs are cut; cut: where those begin, in no order (each of them is joined by itself).
 template <typename Id>
-__global__ void __launch_bounds__(1024) k_embedding_sort(const SortArgs a)
+__global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> a)
 {
     extern __shared__ unsigned smem[];
-    pdl_wait();
+    pdl_begin();
     const unsigned bins = 1u << a.bits, threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
     const Id* ids = static_cast<const Id*>(a.ids);
     if (thread == 0u) a.count[1] = 0u;                               // like `end`, before the first pass
@@ -235,10 +235,10 @@ __device__ __forceinline__ void put_gradient(const TableArgs& a, void* row, int 
 // Blocks below part_blocks add the parts of cut runs; the others take one chunk of `each` table rows per group of threads,
 // whose runs are fetched together: most rows of a large vocabulary have none, and are only written.
 template <int DT, int GT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
+__global__ void __launch_bounds__(256) k_embedding_rows(const Padded<TableArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
-    pdl_wait();
+    pdl_begin();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     Two acc[kPacks][E / 2];
     if (blockIdx.x < a.part_blocks) {
@@ -321,10 +321,10 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const TableArgs a)
 // Joins the parts of the cut runs, 128 columns of one run at a time: eight warps take its parts in turn, and are added in order.
 constexpr unsigned kJoinColumns = 128;
 template <int GT>
-__global__ void __launch_bounds__(256) k_embedding_join(const TableArgs a)
+__global__ void __launch_bounds__(256) k_embedding_join(const Padded<TableArgs> a)
 {
     __shared__ float4 sum[8][32];
-    pdl_wait();
+    pdl_begin();
     const unsigned slice = threadIdx.x >> 5, lane = threadIdx.x & 31u, chunks = (a.hidden + kJoinColumns - 1u) / kJoinColumns;
     const unsigned long long todo = (unsigned long long)a.count[1] * chunks;
     for (unsigned long long t = blockIdx.x; t < todo; t += gridDim.x) {

@@ -18,10 +18,10 @@ struct ExpertSortArgs {
 };
 
 template <typename Id>
-__global__ void __launch_bounds__(1024) k_expert_sort(const ExpertSortArgs a)
+__global__ void __launch_bounds__(1024) k_expert_sort(const Padded<ExpertSortArgs> a)
 {
     extern __shared__ unsigned smem[];
-    pdl_wait();
+    pdl_begin();
     unsigned* counts = smem;                                         // [num_experts]
     const unsigned threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
     const Id* ids = static_cast<const Id*>(a.experts);
@@ -103,11 +103,11 @@ __device__ __forceinline__ void zero_empty_rows(const MoveArgs& a)
 // Every token's row to its pairs' rows.  Whole vectors are read once; rows that are cut otherwise are cut as each of the rows
 // that are written, and read again for each (from L1).
 template <int DT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
+__global__ void __launch_bounds__(256) k_expert_dispatch(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
     constexpr int kAhead = kWhole ? 8 : 4;                           // rows of the map that are fetched together
-    pdl_wait();
+    pdl_begin();
     if (blockIdx.x < a.zero_blocks) {
         zero_empty_rows<DT, kWhole>(a);
     } else {
@@ -162,11 +162,11 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(const MoveArgs a)
 }
 
 template <int DT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
+__global__ void __launch_bounds__(256) k_expert_combine(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
     constexpr int kAhead = kWhole && kPacks == 1 ? 8 : 4;            // expert rows in flight
-    pdl_wait();
+    pdl_begin();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;
     if (unit < a.units) {
@@ -224,12 +224,12 @@ __global__ void __launch_bounds__(256) k_expert_combine(const MoveArgs a)
 // A token per group of threads, which goes over the row kPacks pieces a thread at a time; kBatch pairs' products are summed
 // together, and over the group at the end of the row.
 template <int DT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_expert_combine_backward(const MoveArgs a)
+__global__ void __launch_bounds__(256) k_expert_combine_backward(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
     constexpr int kBatch = kWhole ? 4 : 2;                           // pairs in flight
     __shared__ float red[2][8][kBatch];
-    pdl_wait();
+    pdl_begin();
     if (blockIdx.x < a.zero_blocks) {
         zero_empty_rows<DT, kWhole>(a);
     } else {

@@ -134,7 +134,7 @@ __host__ __device__ constexpr int norm_threads(int packs, bool vec) { return vec
 __host__ __device__ constexpr int norm_depth(int packs, bool vec) { return !vec ? 2 : packs == 4 ? 2 : 3; }
 
 template <int DT, int PT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(const NormArgs a)
+__global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(const Padded<NormArgs> a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
     constexpr int kDepth = norm_depth(kPacks, kVec);
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
     unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
     RowFetch<DT, kPacks, kVec, 2, kDepth> fetch = {{a.x, a.residual}, {a.x_stride, a.residual_stride}, {true, a.residual != nullptr},
                                                    a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
-    pdl_wait();
+    pdl_begin(a.rows <= step);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
     constexpr int P = kLanes<DT, kVec>;
@@ -228,11 +228,11 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
 
 // Rows longer than a block's registers hold: one block per row, which reads the row again for each of the three steps.
 template <int DT, int PT, bool kVec>
-__global__ void __launch_bounds__(1024) k_norm_forward_long(const NormArgs a)
+__global__ void __launch_bounds__(1024) k_norm_forward_long(const Padded<NormArgs> a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
     __shared__ float red[2][32];
-    pdl_wait();
+    pdl_begin(a.rows <= gridDim.x);
     const unsigned warps = blockDim.x / 32u;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const void* x = row_at(a.x, row, a.x_stride);
@@ -294,7 +294,7 @@ __host__ __device__ constexpr int norm_grad_threads(bool vec) { return vec ? 512
 __host__ __device__ constexpr int norm_grad_depth(int packs, bool vec) { return !vec && packs > 4 ? 1 : packs == 1 ? 4 : 2; }
 
 template <int DT, int PT, int kPacks, bool kVec>
-__global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const NormGradArgs a)
+__global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const Padded<NormGradArgs> a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
     constexpr int kDepth = norm_grad_depth(kPacks, kVec);
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
     unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
     RowFetch<DT, kPacks, kVec, 3, kDepth> fetch = {{a.x, a.dy, a.dsummed}, {a.x_stride, a.dy_stride, a.dsummed_stride}, {true, true, a.dsummed != nullptr},
                                                    a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
-    pdl_wait();
+    pdl_begin(a.rows <= step);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
     constexpr int P = kLanes<DT, kVec>;
@@ -446,11 +446,11 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
 
 // Rows longer than a block's registers hold; the block's shares are kept in the workspace from row to row.
 template <int DT, int PT, bool kVec>
-__global__ void __launch_bounds__(1024) k_norm_backward_long(const NormGradArgs a)
+__global__ void __launch_bounds__(1024) k_norm_backward_long(const Padded<NormGradArgs> a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
     __shared__ float red[2][64];
-    pdl_wait();
+    pdl_begin(a.rows <= gridDim.x);
     const unsigned warps = blockDim.x / 32u;
     float* share = a.part ? a.part + (size_t)blockIdx.x * 2u * a.part_stride : nullptr;
     unsigned turn = 0;
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(8 * kSlices) k_norm_params(const float* part, 
 {
     constexpr int kEach = (int)(kNormBlocks + kSlices - 1) / kSlices;
     __shared__ float sum[kSlices][33];
-    pdl_wait();
+    pdl_begin();
     const unsigned which = blockIdx.x / column_blocks, column = blockIdx.x % column_blocks * 32u, slice = threadIdx.x / 8u, at = threadIdx.x % 8u * 4u;
     void* out = which ? dbias : dweight;
     if (out == nullptr) return;
@@ -578,13 +578,17 @@ static int forward(const nuna_layernorm_t& n, unsigned flags, void* stream)
         };
         using Yes = std::true_type;
         using No = std::false_type;
-        // Few rows: as many threads as a row has vectors, for its latency (1 x 8192 bf16 3.3 us, 4.8 with four vectors a thread).
+        // Few rows: 256 threads a row, of which fewer have more to add and more have more sums to exchange (1 x 8192 bf16 with
+        // 1024 | 512 | 256 threads 3.15 | 3.01 | 2.84 us, 1 x 2048 with 256 | 128 | 64 1.95 | 2.27 | 2.64).
         // Many: four vectors a thread, so that a warp's part in the sums (40 instructions) is small beside its elements, and two
         // blocks, each of which works while the other one sums (4096 x 8192 bf16 without residual 25.0 us; two vectors a
         // thread in one block 37).  With a residual it is the four streams' traffic that bounds long rows, and fewer rows at a
         // time are ahead: one block with two vectors a thread, where its groups fill it (4096 x 8192 44.4 against 47.1 us, 8192
         // x 4096 44.1 | 46.8; but 32768 x 1024 55 | 46.4).
-        if (vec && (a.packs <= 32 || (a.packs <= 1024 && a.rows <= 2 * kSms))) return run(Num<1>{}, Yes{}, 256, 1024);
+        const bool few = a.rows <= 2 * kSms;
+        if (vec && (a.packs <= 32 || (few && a.packs <= 256))) return run(Num<1>{}, Yes{}, 256, 1024);
+        if (vec && few && a.packs <= 512) return run(Num<2>{}, Yes{}, 256, 1024);
+        if (vec && few && a.packs <= 2048) return run(Num<4>{}, Yes{}, 256, 512);
         if (vec && a.residual && a.packs >= 480 && a.packs <= 1024 && 512u % group_for(a.packs, 2) == 0u) return run(Num<2>{}, Yes{}, 512, 512);
         if (vec && a.packs <= 64) return run(Num<2>{}, Yes{}, 256, 512);
         if (vec && a.packs <= 2048) return run(Num<4>{}, Yes{}, 256, 512);
@@ -637,7 +641,7 @@ static int backward(const nuna_layernorm_grad_t& n, unsigned flags, void* stream
     if (st != NUNA_OK || !params || (accumulate && n.rows == 0)) return st;
     const unsigned column_blocks = (a.hidden + 31u) / 32u;
     return with_dtype(n.param_dtype, [&](auto pt) {
-        return launch_op(k_norm_params<decltype(pt)::value>, Shape{2 * column_blocks, 8 * kSlices, 0, 1}, flags, stream, a.part, n.dweight, n.dbias, shares,
+        return launch_kernel(k_norm_params<decltype(pt)::value>, Shape{2 * column_blocks, 8 * kSlices, 0, 1}, flags, stream, a.part, n.dweight, n.dbias, shares,
                          a.hidden, a.part_stride, column_blocks, accumulate);
     });
 }

@@ -48,13 +48,21 @@ struct VectorRows {
     }
 };
 
+// Kernel arguments, filled up to 32 bytes beyond a multiple of 64: see ParamPad.
+template <typename T, size_t kPad = (96 - sizeof(T) % 64) % 64>
+struct Padded : T {
+    unsigned char unused[kPad];
+};
+template <typename T>
+struct Padded<T, 0> : T {};
+
 struct Shape {
     unsigned grid, block, smem, cluster;
 };
 
 // Launches an operator's kernel, as a dependent launch if the flags say so (effective_flags has been asked).
 template <typename... Args, typename... Act>
-int launch_op(void (*kernel)(Args...), const Shape& sh, unsigned flags, void* stream, Act&&... args)
+int launch_kernel(void (*kernel)(Args...), const Shape& sh, unsigned flags, void* stream, Act&&... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sh.grid, 1, 1);
@@ -83,6 +91,15 @@ int launch_op(void (*kernel)(Args...), const Shape& sh, unsigned flags, void* st
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return NUNA_OK;
+}
+
+template <typename T>
+int launch_op(void (*kernel)(Padded<T>), const Shape& sh, unsigned flags, void* stream, const T& args)
+{
+    static_assert(sizeof(Padded<T>) % 64 == 32, "see ParamPad");
+    Padded<T> a = {};
+    static_cast<T&>(a) = args;
+    return launch_kernel(kernel, sh, flags, stream, a);
 }
 
 // Raises the kernel's limit of dynamic shared memory, once per device.
@@ -114,6 +131,15 @@ int with_dtype(int dtype, F&& f)
 }
 
 // ---- device ----------------------------------------------------------------------------------------
+
+// What every operator's kernel begins with.  A short grid (`brief`: its blocks do not loop) that leaves SMs free releases its
+// successor at once: the slots that the waiting blocks take are not missed, and their launch is out of the way when this grid
+// ends (norm of 1 x 8192 3.5 -> 3.15 us; 4096 rows in 148 looping blocks 45.7 -> 46.6, which is why they do not).
+__device__ __forceinline__ void pdl_begin(bool brief = true)
+{
+    if (brief && gridDim.x <= kSms) pdl_trigger();
+    pdl_wait();
+}
 
 // A pack is what a thread moves at once: a 16-byte vector, or (rows of any length and alignment) one element.
 template <int DT, bool kVec> struct Pack {

@@ -34,13 +34,9 @@ constexpr int kMaxFields = 28;
 PyObject* g_tail[3] = {};
 const char* const kTail[3] = {"flags", "stream", "check"};
 
-bool fits_device(const at::Tensor& t)
-{
-    return t.is_cuda() && t.device().index() == c10::cuda::current_device();
-}
-
-// A buffer's address and how many bytes it has from there on (all, if it does not say).
-bool buffer_of(PyObject* x, void** at, size_t* bytes, bool* elsewhere)
+// A buffer's address and how many bytes it has from there on (all, if it does not say).  `device`: the current one, asked for
+// with the first tensor (-1 before).
+bool buffer_of(PyObject* x, void** at, size_t* bytes, int* device, bool* elsewhere)
 {
     *bytes = SIZE_MAX;
     if (x == Py_None) {
@@ -51,8 +47,12 @@ bool buffer_of(PyObject* x, void** at, size_t* bytes, bool* elsewhere)
     try {
         const at::Tensor& t = THPVariable_Unpack(x);
         *at = t.mutable_data_ptr();
-        if (*at) *elsewhere = *elsewhere || !fits_device(t);
-        const size_t all = t.storage().nbytes(), before = (size_t)t.storage_offset() * t.element_size();
+        if (*at) {
+            if (*device < 0 && t.is_cuda()) *device = c10::cuda::current_device();
+            *elsewhere = *elsewhere || !t.is_cuda() || t.device().index() != *device;
+        }
+        const c10::TensorImpl* impl = t.unsafeGetTensorImpl();
+        const size_t all = impl->unsafe_storage().unsafeGetStorageImpl()->nbytes(), before = (size_t)impl->storage_offset() * impl->itemsize();
         *bytes = all > before ? all - before : 0;
         return true;
     } catch (const std::exception& e) {
@@ -133,6 +133,7 @@ PyObject* run(Op<Args>& op, Args a, PyObject* const* args, Py_ssize_t npos, PyOb
     size_t has[nuna::kMaxSpans];
     for (size_t& h : has) h = SIZE_MAX;
     bool elsewhere = false, sized = false;
+    int device = -1;
     char* base = reinterpret_cast<char*>(&a);
     for (int i = 0; i < op.n; ++i) {
         const Field& f = op.field[i];
@@ -142,7 +143,7 @@ PyObject* run(Op<Args>& op, Args a, PyObject* const* args, Py_ssize_t npos, PyOb
         }
         if (f.kind == kBuffer) {
             void* at = nullptr;
-            if (!buffer_of(given[i], &at, &has[f.span], &elsewhere)) return nullptr;
+            if (!buffer_of(given[i], &at, &has[f.span], &device, &elsewhere)) return nullptr;
             memcpy(base + f.at, &at, sizeof at);
         } else {
             if (!put(given[i], f, base + f.at)) return nullptr;

@@ -89,7 +89,10 @@ struct SortArgs {
     unsigned *begin, *end, *count, *cut;
     long long vocab_start;
     unsigned tokens, vocab_rows, passes, bits;                       // bits of a digit
+    unsigned sorters;                                                // blocks that sort; the others zero the table
     bool clear;                                                      // rows without a token get end = 0
+    uint4* zero;
+    unsigned long long zero_vectors;
 };
 
 // items[passes & 1 ^ 1]: the tokens with a row in the slice, by row and then by token; begin / end: each row's run; count: how
@@ -98,8 +101,17 @@ template <typename Id>
 __global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> a)
 {
     extern __shared__ unsigned smem[];
-    pdl_begin();
-    const unsigned bins = 1u << a.bits, threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
+    pdl_begin(a.sorters == gridDim.x);
+    if (blockIdx.x >= a.sorters) {
+        // a stretch of its own for every block
+        const unsigned blocks = gridDim.x - a.sorters;
+        const unsigned long long each = (a.zero_vectors + blocks - 1u) / blocks, from = (blockIdx.x - a.sorters) * each;
+        const unsigned long long to = from + each < a.zero_vectors ? from + each : a.zero_vectors;
+#pragma unroll 4
+        for (unsigned long long i = from + threadIdx.x; i < to; i += blockDim.x) st_stream(a.zero + i, make_uint4(0u, 0u, 0u, 0u));
+        return;
+    }
+    const unsigned bins = 1u << a.bits, threads = a.sorters * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
     const Id* ids = static_cast<const Id*>(a.ids);
     if (thread == 0u) a.count[1] = 0u;                               // like `end`, before the first pass
     if (a.clear)                                                     // whose barriers order it
@@ -110,7 +122,7 @@ __global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> 
         return id >= a.vocab_start && from < a.vocab_rows ? (unsigned)from : kNoDigit;
     };
     uint2 *to = a.items[0], *from = a.items[1];
-    const unsigned n = sort_pass<long long>(a.tokens, bins, smem, nullptr,
+    const unsigned n = sort_pass<long long>(a.sorters, a.tokens, bins, smem, nullptr,
         [&](unsigned i) { return load_id(ids + i); },
         [&](long long id) {
             const unsigned row = row_of(id);
@@ -122,7 +134,7 @@ __global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> 
     for (unsigned pass = 1; pass < a.passes; ++pass) {
         uint2* last = to;
         to = from, from = last;
-        sort_pass<uint2>(n, bins, smem, nullptr, [&](unsigned i) { return load_shared_by_cluster(from + i); },
+        sort_pass<uint2>(a.sorters, n, bins, smem, nullptr, [&](unsigned i) { return load_shared_by_cluster(from + i); },
             [&](uint2 item) { return (item.y >> (pass * a.bits)) & (bins - 1u); },
             [&](unsigned, uint2 item, unsigned, unsigned first, unsigned rank) { to[first + rank] = item; });
     }
@@ -144,11 +156,12 @@ struct TableArgs {
     const unsigned *begin, *end, *count, *cut;
     float* part;                                                     // [parts][2][part_stride]
     size_t dout_stride, dtable_stride;                               // bytes
-    unsigned rows, row_units, each;                                  // table rows (positions, if accumulating); (rows / each) * chunks
+    unsigned rows, row_units, each;                                  // table rows (positions, if by_position); (rows / each) * chunks
     unsigned parts, part_blocks;                                     // cuts of the positions, blocks that add them
     unsigned tokens, hidden, chunks, group, part_stride;
     float scale;
-    bool accumulate, whole_sectors;                                  // rows of dtable are at 32-byte addresses
+    bool accumulate, by_position;                                    // by_position: rows without a token are left alone, or zero already
+    bool whole_sectors;                                              // rows of dtable are at 32-byte addresses
 };
 
 // acc += pieces from + k * group, which begin at E times that minus s, of the rows of dout that positions p ... end-1 name, in
@@ -235,7 +248,7 @@ __device__ __forceinline__ void put_gradient(const TableArgs& a, void* row, int 
 // Blocks below part_blocks add the parts of cut runs; the others take one chunk of `each` table rows per group of threads,
 // whose runs are fetched together: most rows of a large vocabulary have none, and are only written.
 template <int DT, int GT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_embedding_rows(const Padded<TableArgs> a)
+__global__ void __launch_bounds__(256, 3) k_embedding_rows(const Padded<TableArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
     pdl_begin();
@@ -274,7 +287,7 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const Padded<TableArgs> 
             const unsigned first = unit / a.chunks * a.each, from = unit % a.chunks * a.group * kPacks + lane, me = threadIdx.x & 31u;
             unsigned v = first + me, b = 0, e = 0;                   // of the row that this lane looks at
             bool mine = me < a.each && v < a.rows;
-            if (mine && a.accumulate) {                              // a position: the first of a run stands for its row
+            if (mine && a.by_position) {                             // a position: the first of a run stands for its row
                 const unsigned p = v;
                 mine = p < a.count[0];
                 if (mine) v = a.items[p].y, b = a.begin[v], e = a.end[v];
@@ -283,7 +296,9 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const Padded<TableArgs> 
                 e = a.end[v];
                 if (e) b = a.begin[v];
             }
-            const unsigned empty = __ballot_sync(0xFFFFFFFFu, mine && e == b), todo = __ballot_sync(0xFFFFFFFFu, mine && e != b && e - b <= kRunPart);
+            const unsigned only = mine && e - b == 1u ? a.items[b].x : 0u;       // the token of a run of one, as most are
+            const unsigned empty = __ballot_sync(0xFFFFFFFFu, mine && e == b), single = __ballot_sync(0xFFFFFFFFu, mine && e - b == 1u),
+                           todo = __ballot_sync(0xFFFFFFFFu, mine && e - b > 1u && e - b <= kRunPart);
             // Rows without a token: one after the other, they are only stores, of consecutive vectors by consecutive lanes.
             constexpr int G = Elem<GT>::kElems, kParts = E / G;
             const Pack<GT, true> zero = {};
@@ -296,6 +311,41 @@ __global__ void __launch_bounds__(256) k_embedding_rows(const Padded<TableArgs> 
                     const int e0 = (int)((zero_from + k * a.group) * G) - s;
                     if (touches<G>(e0, a.hidden)) store_piece<GT, kWhole, true>(row, a.hidden, e0, zero);
                 }
+            }
+            // Rows with one token: several at a time.
+            constexpr int kRows = 4;
+            for (unsigned left = single; left;) {
+                Piece<DT, kWhole> p[kRows][kPacks];
+                Source source[kRows];
+                void* row[kRows];
+                int s[kRows], n = 0;
+#pragma unroll
+                for (int q = 0; q < kRows; ++q) {
+                    const int r = left ? __ffs(left) - 1 : 0;
+                    const unsigned row_v = __shfl_sync(0xFFFFFFFFu, v, r), token = __shfl_sync(0xFFFFFFFFu, only, r);
+                    if (left) {
+                        left &= left - 1u;
+                        ++n;
+                        row[q] = row_at(a.dtable, row_v, a.dtable_stride);
+                        s[q] = kWhole ? 0 : behind<GT, E>(row[q]);
+                        source[q] = source_of<DT, kWhole>(a.dout, token, a.dout_stride, a.tokens, a.hidden, s[q]);
+#pragma unroll
+                        for (int k = 0; k < kPacks; ++k) {
+                            const int e0 = (int)((from + k * a.group) * E) - s[q];
+                            if (touches<E>(e0, a.hidden)) fetch_piece<DT, kWhole>(p[q][k], source[q], from + k * a.group, e0, a.hidden);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < kRows; ++q)
+                    if (q < n)
+#pragma unroll
+                        for (int k = 0; k < kPacks; ++k) {
+                            const int e0 = (int)((from + k * a.group) * E) - s[q];
+                            Two f[E / 2];
+                            unpack<DT, true>(f, settle_piece<DT, kWhole>(p[q][k], source[q]));
+                            if (touches<E>(e0, a.hidden)) put_gradient<GT, E, kWhole>(a, row[q], e0, f);
+                        }
             }
             for (unsigned left = todo; left; left &= left - 1u) {
                 const int r = __ffs(left) - 1;
@@ -405,6 +455,8 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
     return with_dtype(n.dtype, [&](auto dt) { return n.id_bytes == 8 ? typed((long long)0, dt) : typed(0, dt); });
 }
 
+constexpr size_t kZeroBytes = 384 << 10;                             // that a block zeroes, about: 7.2 TB/s; with 113 KB and 3.6 MB 7.0 and 6.5
+
 static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* stream)
 {
     const size_t e = dtype_bytes(n.dtype), ge = dtype_bytes(n.grad_dtype);
@@ -414,7 +466,15 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     const auto words = [&](size_t at) { return reinterpret_cast<unsigned*>(static_cast<char*>(n.workspace) + at); };
     SortArgs s = {};
     s.ids = n.ids, s.vocab_start = n.vocab_start, s.tokens = (unsigned)n.tokens, s.vocab_rows = (unsigned)n.vocab_rows;
-    s.clear = !accumulate;
+    // Few tokens beside the table's rows: one block sorts, the others zero the table meanwhile, and only rows with a token are
+    // visited (8192 tokens, a quarter of them in the slice of 32768 x 4096 f32: 94.7 us against 103; 1000 tokens, 50000 x 1024: 40 | 50;
+    // 128 tokens, 4096 x 4096: 15 | 19).  With more tokens too much is written twice (8192 tokens to 32768 rows 116 | 114), or the
+    // sort outlasts the stores (3 ns a token in one block).
+    const bool vec = VectorRows{true}.rows(n.dout, n.hidden, n.dout_stride, e).rows(n.dtable, n.hidden, n.dtable_stride, ge).ok;
+    const bool whole = n.dtable_stride == 0 || n.dtable_stride == n.hidden;
+    const bool zero_first = !accumulate && vec && whole && n.tokens && n.tokens * 4 <= n.vocab_rows && n.tokens <= 16384 &&
+                            n.vocab_rows * n.hidden * ge >= n.tokens * (24 << 10);
+    s.clear = !accumulate && !zero_first;
     for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint2*>(words(w.items[i]));
     s.begin = words(w.begin), s.end = words(w.end), s.count = words(w.count), s.cut = words(w.cut);
     unsigned bits = 1;
@@ -422,7 +482,15 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     s.passes = (bits + 9u) / 10u;                                    // digits of at most 10 bits: 1024 bins a warp fit a block's shared memory
     s.bits = (bits + s.passes - 1u) / s.passes;
     if (n.tokens) {
-        const Shape sort = sort_shape(n.tokens, 1u << s.bits);
+        Shape sort = sort_shape(n.tokens, 1u << s.bits);
+        s.sorters = sort.grid;
+        if (zero_first) {
+            s.zero = static_cast<uint4*>(n.dtable), s.zero_vectors = n.vocab_rows * n.hidden * ge / 16;
+            s.sorters = 1;                                           // the sort is hidden: a cluster would only leave SMs without a block
+            const size_t wave = (kSms - 1) * kZeroBytes;             // one of these blocks is resident on an SM
+            const unsigned blocks = (kSms - 1) * (unsigned)std::max<size_t>(1, (n.vocab_rows * n.hidden * ge + wave / 2) / wave);
+            sort = Shape{1 + blocks, kSortMaxWarps * 32u, sort_smem(kSortMaxWarps, 1u << s.bits), 1};
+        }
         constexpr int kMost = sort_smem(kSortMaxWarps, 1024);
         const bool wide = n.id_bytes == 8;
         int st = wide ? allow_sort<k_embedding_sort<long long>>(sort, kMost) : allow_sort<k_embedding_sort<int>>(sort, kMost);
@@ -430,7 +498,6 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
         if ((st = launch_op(wide ? k_embedding_sort<long long> : k_embedding_sort<int>, sort, flags, stream, s)) != NUNA_OK) return st;
     }
 
-    const bool vec = VectorRows{true}.rows(n.dout, n.hidden, n.dout_stride, e).rows(n.dtable, n.hidden, n.dtable_stride, ge).ok;
     TableArgs a = {};
     a.dout = n.dout, a.dtable = n.dtable;
     a.items = s.items[(s.passes & 1u) ^ 1u], a.begin = s.begin, a.end = n.tokens ? s.end : nullptr, a.count = s.count, a.cut = s.cut;
@@ -440,7 +507,8 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     a.part_stride = (unsigned)part_stride(n.hidden), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     a.scale = n.scale, a.accumulate = accumulate, a.whole_sectors = !(((uintptr_t)n.dtable | a.dtable_stride) & 31u);
     a.parts = n.tokens > kRunPart ? (unsigned)((n.tokens + kRunPart - 1) / kRunPart) : 0u;
-    a.rows = (unsigned)(accumulate ? n.tokens : n.vocab_rows);
+    a.by_position = accumulate || zero_first;
+    a.rows = (unsigned)(a.by_position ? n.tokens : n.vocab_rows);
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const auto run = [&](auto rows, auto join, int per_thread) {
@@ -450,7 +518,7 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
             const auto blocks = [&](unsigned long long units) { return (units + groups - 1) / groups; };
             // as many rows at once as leave each SM 32 warps' work
             a.each = 1;
-            while (a.each < 16u && (unsigned long long)a.rows / (2u * a.each) * sh.chunks * (sh.group / 32u) >= 32ull * kSms) a.each *= 2u;
+            while (a.each < 8u && (unsigned long long)a.rows / (2u * a.each) * sh.chunks * (sh.group / 32u) >= 32ull * kSms) a.each *= 2u;
             const unsigned long long row_units = ((unsigned long long)a.rows + a.each - 1) / a.each * sh.chunks, part_units = (unsigned long long)a.parts * sh.chunks;
             if (row_units > kMaxUnits || part_units > kMaxUnits) return (int)NUNA_ERR_TOO_LARGE;
             a.row_units = (unsigned)row_units;

@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(1024) k_expert_sort(const Padded<ExpertSortArg
     unsigned* counts = smem;                                         // [num_experts]
     const unsigned threads = gridDim.x * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
     const Id* ids = static_cast<const Id*>(a.experts);
-    const unsigned kept = sort_pass<long long>(a.pairs, a.num_experts, smem + a.num_experts, counts,
+    const unsigned kept = sort_pass<long long>(gridDim.x, a.pairs, a.num_experts, smem + a.num_experts, counts,
         [&](unsigned i) { return load_id(ids + i); },
         [&](long long e) {
             const unsigned long long from = (unsigned long long)e - (unsigned long long)a.first_expert;

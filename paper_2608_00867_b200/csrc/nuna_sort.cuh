@@ -76,17 +76,17 @@ __device__ __forceinline__ void sort_sync(unsigned blocks)
     else              cluster_sync();
 }
 
-// One pass over items 0 ... n-1.  load(i): the item (asked twice if a warp has more than 32 * kSortItems of them);
+// One pass over items 0 ... n-1 by the grid's first `blocks` blocks, which are a cluster.  load(i): the item (asked twice if a warp has more than 32 * kSortItems of them);
 // digit(item): its bin, or kNoDigit to drop it; place(i, item, digit, first, rank): called once for every item, in any
 // order; `first` is where its bin begins, `rank` its number within the bin.  `counts` (shared, [bins]), if given, receives what
 // all blocks have of each bin.  Returns the number of items that were not dropped.  All threads of the cluster call; shared
 // memory may be reused, and what place() wrote to global memory is visible to the whole cluster, when it returns.
 template <typename Item, typename Load, typename Digit, typename Place>
-__device__ __forceinline__ unsigned sort_pass(unsigned n, unsigned bins, unsigned* smem, unsigned* counts, Load load, Digit digit, Place place)
+__device__ __forceinline__ unsigned sort_pass(unsigned blocks, unsigned n, unsigned bins, unsigned* smem, unsigned* counts, Load load, Digit digit, Place place)
 {
     __shared__ unsigned red[32];
     const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const unsigned blocks = gridDim.x, block = blockIdx.x;                       // the grid is the cluster
+    const unsigned block = blockIdx.x;
     unsigned *hist = smem, *totals = hist + warps * bins, *first = totals + bins, *ahead = first + bins, *segment = ahead + bins;
     const unsigned parts = blocks * warps;
     const unsigned per_warp = (unsigned)(((unsigned long long)n + parts * 32ull - 1ull) / (parts * 32ull) * 32ull);

@@ -416,16 +416,17 @@ int nuna_chain_destroy(void* chain);
  *    device, aligned to their element type (rows that are 16-byte aligned and a whole number of 16-byte vectors
  *    long are faster).  An optional pointer is NULL where it is not wanted.
  *  - Matrices are rows of `hidden` contiguous elements; *_stride is the distance between rows in elements (at
- *    least `hidden`; 0 = `hidden`).  What lies between the rows is neither read nor written.
+ *    least `hidden`; 0 = `hidden`).  What lies between the rows is not written, and nothing that is read of it is used
+ *    (a row is read as the 16-byte vectors that hold it; never beyond a matrix's first and last byte).
  *  - Calls are asynchronous on `stream` and allocate nothing; workspaces belong to the caller (two calls that may
  *    overlap, captured graphs among them, need two), and the first call on a device may be a captured one.
  *    `flags`: NUNA_LAUNCH_PDL and, where said, NUNA_GRAD_ACCUMULATE.
  *  - No written range may overlap another range of the call (NUNA_ERR_ALIAS) but where said; a range reaches from
  *    a matrix's first byte to its last, the gaps between rows included.
- *  - Sizes are at most 2^31 - 1 rows, tokens, table rows, pairs or elements in a row, and 2^46 bytes a matrix
+ *  - Sizes are at most 2^31 - 1 rows, tokens, table rows or pairs, 2^30 elements in a row and 2^46 bytes a matrix
  *    (NUNA_ERR_TOO_LARGE).  Sizes of zero are valid: outputs that a sum over nothing defines are written.
- *  - Arithmetic is binary32 whatever the element type, in an order that sizes and types alone decide, with one
- *    rounding at the end: the same call gives the same bits.                                                  */
+ *  - Arithmetic is binary32 whatever the element type, in an order that sizes, types and alignments decide, with
+ *    one rounding at the end: the same call gives the same bits.                                               */
 
 /* `flags`, bit 15: gradients of parameters (dweight, dbias, dtable) are added to what their buffers hold (in
  * binary32, rounded once) instead of replacing it.                                                           */
@@ -497,7 +498,7 @@ int nuna_embedding_forward(const nuna_embedding_t* args, unsigned flags, void* s
  * every row is written, rows without a token with zeros.  With NUNA_GRAD_ACCUMULATE the sum is added to
  * dtable[v], and rows without a token are neither read nor written.  grad_dtype (of dtable): dtype or NUNA_F32.
  * The tokens are sorted by id first, so the sum's order is fixed.  workspace: nuna_embedding_workspace bytes,
- * 16-byte aligned.                                                                                           */
+ * 32-byte aligned.                                                                                           */
 typedef struct nuna_embedding_grad {
     size_t tokens, hidden, vocab_rows;
     const void* ids;
@@ -538,7 +539,8 @@ int nuna_expert_sort(const nuna_expert_sort_t* args, unsigned flags, void* strea
 
 /* out[row_of_pair[t * topk + j]] = x[t], bit for bit.  With pair_of_row, rows whose entry is -1 are zeroed (what an
  * alltoall sends); without it rows that no pair has stay as they are.  rows: rows of `out`; an entry of row_of_pair
- * outside [0, rows) is a dropped pair here and below.                                                         */
+ * outside [0, rows) is a dropped pair here and below.  No two pairs may have the same row here and in
+ * nuna_expert_combine_backward (nuna_expert_sort gives none two): what it then holds is not defined.            */
 typedef struct nuna_expert_dispatch {
     size_t tokens, topk, rows, hidden;
     const void* x;

@@ -291,7 +291,7 @@ __device__ __forceinline__ void* row_at(void* base, size_t row, size_t stride_by
 // own 16-byte boundaries: piece i is the E elements from E * i - s on, s being how far behind a boundary the row begins.  All
 // pieces but the first and the last are then stored as vectors.  A row that is read lies at some other distance from a boundary,
 // the same for all of its pieces: a piece is shifted out of the two vectors around it, 2 loads and 4 shifts instead of E loads
-// (lookup of 20011 rows of 1037 f16: 26.5 -> 20 us).  Those two vectors may reach up to 14 bytes beyond the row, into its
+// (lookup of 20011 rows of 1037 f16: 26.5 -> 23.6 us).  Those two vectors may reach up to 14 bytes beyond the row, into its
 // neighbours or the gaps; what comes from there is not used, and the first and the last row of a matrix, where nothing need be
 // there, are read element by element.
 template <int DT, bool kWhole> struct Piece {

@@ -8,7 +8,8 @@
 
 namespace nuna {
 
-constexpr size_t kMaxExtent = (size_t)0x7FFFFFFF;        // rows, tokens, table rows, elements in a row
+constexpr size_t kMaxExtent = (size_t)0x7FFFFFFF;        // rows, tokens, table rows
+constexpr size_t kMaxHidden = (size_t)1 << 30;           // elements in a row: a 32-bit index may step beyond its end
 constexpr size_t kMaxMatrixBytes = (size_t)1 << 46;
 constexpr int kMaxSpans = 10;
 
@@ -28,6 +29,14 @@ struct Spans {
 
     // rows of `elems` elements of `size` bytes, `stride` elements apart (0: elems)
     void matrix(const void* at, size_t rows, size_t elems, size_t stride, size_t size, bool written, bool required = true)
+    {
+        if (elems > kMaxHidden) fail(NUNA_ERR_TOO_LARGE);
+        extent(at, rows, elems, stride, size, written, required);
+    }
+    void array(const void* at, size_t elems, size_t size, bool written, bool required = true) { extent(at, 1, elems, 0, size, written, required); }
+    // `bytes` (a multiple of 32) that kernels write 32 bytes at a time
+    void workspace(const void* at, size_t bytes, bool required) { array(at, bytes / 32, 32, true, required); }
+    void extent(const void* at, size_t rows, size_t elems, size_t stride, size_t size, bool written, bool required)
     {
         Span& s = v[n++];
         s.at = at;
@@ -49,7 +58,6 @@ struct Spans {
         s.stride = stride * size;
         s.bytes = (size_t)bytes;
     }
-    void array(const void* at, size_t elems, size_t size, bool written, bool required = true) { matrix(at, 1, elems, 0, size, written, required); }
     void fail(int st)
     {
         if (status == NUNA_OK) status = st;
@@ -149,7 +157,7 @@ inline Spans spans_of(const nuna_embedding_grad_t& a)
     s.array(a.ids, a.tokens, id_size(a.id_bytes), false, a.tokens != 0);
     s.matrix(a.dout, a.tokens, a.hidden, a.dout_stride, dtype_bytes(a.dtype), false, a.tokens != 0);
     s.matrix(a.dtable, a.vocab_rows, a.hidden, a.dtable_stride, dtype_bytes(a.grad_dtype), true);
-    s.array(a.workspace, embedding_workspace(a.tokens, a.hidden, a.vocab_rows).bytes / 16, 16, true, a.tokens != 0);
+    s.workspace(a.workspace, embedding_workspace(a.tokens, a.hidden, a.vocab_rows).bytes, a.tokens != 0);
     return s;
 }
 

@@ -2,7 +2,7 @@
 //
 // A buffer is a torch tensor, an object with data_ptr(), an address, or None where it is optional.  What a tensor says of
 // itself is held against the call: it has to be on the current device, and its storage, from its first element on, as long as
-// the call's sizes and strides reach.  Measured with the library's own checks and without the launch (hidden 0): 0.6 us.
+// the call's sizes and strides reach.  Measured with the library's own checks and without the launch (hidden 0): 0.45 us.
 #include "nuna_py.h"
 
 #include <c10/cuda/CUDAFunctions.h>

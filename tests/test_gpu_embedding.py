@@ -11,7 +11,8 @@ pytestmark = pytest.mark.gpu
 # (tokens, hidden, rows of the slice, its start, the vocabulary)
 SHAPES = [(1, 1, 1, 0, 1), (1, 8, 5, 0, 5), (3, 7, 4, 2, 9), (64, 64, 16, 0, 16), (65, 64, 16, 0, 16), (63, 33, 1, 0, 1), (129, 40, 1, 0, 2),
           (1000, 256, 37, 100, 200), (257, 1024, 1000, 0, 1000), (500, 1037, 300, 17, 400), (2500, 520, 3, 0, 3), (300, 8192, 50, 0, 64),
-          (8193, 72, 1025, 0, 1025), (20000, 24, 131072, 0, 131072), (70000, 16, 2049, 5, 3000), (37, 16392, 9, 0, 9), (4, 65537, 3, 0, 4)]
+          (8193, 72, 1025, 0, 1025), (20000, 24, 131072, 0, 131072), (70000, 16, 2049, 5, 3000), (37, 16392, 9, 0, 9), (4, 65537, 3, 0, 4),
+          (150000, 8, 40000, 0, 40000), (300, 520, 5000, 100, 6000), (5000, 4096, 30000, 0, 60000), (16390, 40, 70000, 0, 70000)]
 IDS = {"i32": torch.int32, "i64": torch.int64}
 
 
@@ -158,6 +159,51 @@ def test_not_finite_values_stay_in_their_rows():
     ws = torch.empty(nb.nuna_embedding_workspace(6, 1, 4), dtype=torch.uint8, device="cuda")
     nb.nuna_embedding_backward(ids, dout, grad, 6, 1, 4, workspace=ws, dtype=nb.NUNA_F32, grad_dtype=nb.NUNA_F32)
     assert grad[:, 0].tolist() == [1.0, float("inf"), 1.0, 1.0]               # what no row of the slice has is not read
+
+
+def test_zeros_of_no_row_are_not_scaled():
+    table = torch.ones(2, 24, device="cuda")
+    for scale, want in ((float("inf"), float("inf")), (0.0, 0.0), (float("nan"), float("nan"))):
+        out = torch.full((3, 24), GUARD, device="cuda")
+        nb.nuna_embedding_forward(torch.tensor([1, 2, -5], device="cuda"), table, out, 3, 24, 2, scale=scale, dtype=nb.NUNA_F32)
+        assert bool((out[1:] == 0).all()) and torch.equal(out[0], torch.full_like(out[0], want)) or want != want and bool(torch.isnan(out[0]).all())
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    code = """
+import torch
+from paper_2608_00867_b200 import binding as nb
+f32 = dict(dtype=nb.NUNA_F32)
+i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+tokens, hidden, rows = 20000, 256, 300
+ids = torch.arange(tokens, device="cuda") % rows
+table, out, grad = torch.randn(rows, hidden, device="cuda"), torch.zeros(tokens, hidden, device="cuda"), torch.zeros(rows, hidden, device="cuda")
+y, mean, rstd, dx, dw = torch.zeros_like(out), torch.zeros(tokens, device="cuda"), torch.zeros(tokens, device="cuda"), torch.zeros_like(out), torch.zeros(hidden, device="cuda")
+row, pair, offsets, moved, back = i32(tokens), i32(tokens), i32(301), torch.zeros_like(out), torch.zeros_like(out)
+ws = torch.empty(nb.nuna_embedding_workspace(tokens, hidden, rows), dtype=torch.uint8, device="cuda")
+wn = torch.empty(nb.nuna_layernorm_workspace(tokens, hidden), dtype=torch.uint8, device="cuda")
+g = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(g):
+    nb.nuna_embedding_forward(ids, table, out, tokens, hidden, rows, **f32)
+    nb.nuna_layernorm_forward(out, y, tokens, hidden, mean=mean, rstd=rstd, param_dtype=nb.NUNA_F32, **f32)
+    nb.nuna_layernorm_backward(y, out, mean, rstd, dx, tokens, hidden, dweight=dw, workspace=wn, param_dtype=nb.NUNA_F32, **f32)
+    nb.nuna_expert_sort(ids, row, pair, offsets, tokens, 1, 300)
+    nb.nuna_expert_dispatch(y, row, moved, tokens, 1, tokens, hidden, **f32)
+    nb.nuna_expert_combine(moved, row, back, tokens, 1, tokens, hidden, **f32)
+    nb.nuna_embedding_backward(ids, torch.ones_like(out), grad, tokens, hidden, rows, workspace=ws, grad_dtype=nb.NUNA_F32, **f32)
+g.replay()
+torch.cuda.synchronize()
+assert torch.equal(out, table[ids]) and torch.equal(back, y) and float(y.abs().max()) > 0
+assert torch.equal(grad.sum(1), torch.bincount(ids, minlength=rows) * float(hidden))
+assert torch.equal(pair.long(), torch.argsort(ids, stable=True))
+"""
+    import os
+    import subprocess
+    import sys
+    done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True,
+                          text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def test_empty_calls_that_write():

@@ -4,7 +4,7 @@ gradients, against the same path in 64 bits."""
 import pytest
 import torch
 
-from operator_cases import U, generator, half_step, integers, normal, within
+from operator_cases import DTYPES, U, generator, half_step, integers, normal, within
 from paper_2608_00867_b200 import binding as nb
 
 pytestmark = pytest.mark.gpu
@@ -20,7 +20,7 @@ def zeros(*shape, dtype=torch.float32):
 @pytest.mark.parametrize("flags", [0, nb.NUNA_LAUNCH_PDL])
 @pytest.mark.parametrize("graph", [False, True])
 def test_lookup_allreduce_norm_and_back(flags, graph):
-    """Each rank holds a tenth of the vocabulary; ranks 0 ... 7 cover all of it."""
+    """Each rank holds an eighth of the vocabulary."""
     gen = generator(1)
     per = VOCAB // RANKS
     ids = torch.randint(0, VOCAB, (TOKENS,), generator=gen, device="cuda")
@@ -130,3 +130,56 @@ def test_tokens_to_experts_on_other_ranks_and_back(dtype):
             assert bool((send[r][e * CAPACITY + n:(e + 1) * CAPACITY] == 0).all())
     assert dropped > 0
     assert half_step(tdt) > 0 and nb.nuna_device_status() == nb.NUNA_OK
+
+
+@pytest.mark.parametrize("pad,shift", [(3, 0), (1, 1), (11, 5)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gaps_that_hold_nan_change_nothing(dtype, pad, shift):
+    """Rows of an odd length with NaN between and around them give, bit for bit, what rows without gaps give.  Integers and halves, so
+    that sums are exact whatever the rows' addresses."""
+    tdt, code = DTYPES[dtype]
+    tokens, hidden, rows, topk, experts = 61, 37, 23, 3, 8
+    pairs = tokens * topk
+    gen = generator(5, pad)
+    ids = torch.randint(-2, rows + 2, (tokens,), generator=gen, device="cuda")
+    choices = torch.randint(0, experts + 1, (tokens, topk), generator=gen, device="cuda")
+    weights = integers(gen, 1, 4, tokens, topk) * 0.5
+    values = {n: integers(gen, -3, 3, r, hidden) for n, r in dict(table=rows, x=tokens, residual=tokens, dy=tokens, src=pairs).items()}
+    row, pair, offsets = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (pairs, pairs, experts + 1))
+    nb.nuna_expert_sort(choices, row, pair, offsets, tokens, topk, experts)
+
+    def run(pad, shift):
+        stride = hidden + pad
+
+        def rows_of(values, count=None):
+            n = count or values.shape[0]
+            whole = torch.full((shift + n * stride + 64,), float("nan"), dtype=tdt, device="cuda")
+            v = torch.as_strided(whole, (n, hidden), (stride, 1), shift)
+            if count is None:
+                v.copy_(values)
+            return whole[shift:], v
+
+        at = {n: rows_of(v)[0] for n, v in values.items()}
+        out = {n: rows_of(None, c) for n, c in dict(looked=tokens, dtable=rows, summed=tokens, y=tokens, dx=tokens, moved=pairs, back=tokens,
+                                                    dsrc=pairs).items()}
+        to = {n: o[0] for n, o in out.items()}
+        mean, rstd, dw, db, dweights = zeros(tokens), zeros(tokens), zeros(hidden), zeros(hidden), zeros(tokens, topk)
+        ws = zeros(max(nb.nuna_embedding_workspace(tokens, hidden, rows), nb.nuna_layernorm_workspace(tokens, hidden)), dtype=torch.uint8)
+        strides = lambda *names: {f"{n}_stride": stride for n in names}
+        nb.nuna_embedding_forward(ids, at["table"], to["looked"], tokens, hidden, rows, dtype=code, **strides("table", "out"))
+        nb.nuna_embedding_backward(ids, at["dy"], to["dtable"], tokens, hidden, rows, workspace=ws, dtype=code, grad_dtype=code,
+                                   **strides("dout", "dtable"))
+        nb.nuna_layernorm_forward(at["x"], to["y"], tokens, hidden, residual=at["residual"], summed=to["summed"], mean=mean, rstd=rstd,
+                                  dtype=code, param_dtype=nb.NUNA_F32, **strides("x", "residual", "summed", "y"))
+        nb.nuna_layernorm_backward(at["dy"], to["summed"], mean, rstd, to["dx"], tokens, hidden, dsummed=at["x"], dweight=dw, dbias=db,
+                                   workspace=ws, dtype=code, param_dtype=nb.NUNA_F32, **strides("dy", "x", "dsummed", "dx"))
+        nb.nuna_expert_dispatch(at["x"], row, to["moved"], tokens, topk, pairs, hidden, pair_of_row=pair, dtype=code, **strides("x", "out"))
+        nb.nuna_expert_combine(at["src"], row, to["back"], tokens, topk, pairs, hidden, weights=weights, dtype=code, **strides("src", "y"))
+        nb.nuna_expert_combine_backward(at["dy"], at["src"], weights, row, to["dsrc"], dweights, tokens, topk, pairs, hidden,
+                                        pair_of_row=pair, dtype=code, **strides("dy", "src", "dsrc"))
+        torch.cuda.synchronize()
+        return {**{n: o[1].clone() for n, o in out.items()}, "mean": mean, "rstd": rstd, "dw": dw, "db": db, "dweights": dweights}
+
+    want, got = run(0, 0), run(pad, shift)
+    for n in want:
+        assert not bool(torch.isnan(want[n]).any()) and torch.equal(want[n], got[n]), (n, dtype, pad, shift)

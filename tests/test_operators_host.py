@@ -72,6 +72,7 @@ def test_types_flags_and_sizes(name):
         assert status(name, dtype=3) == nb.NUNA_ERR_UNSUPPORTED_DTYPE
         assert status(name, dtype=-1) == nb.NUNA_ERR_UNSUPPORTED_DTYPE
         assert status(name, hidden=HUGE) == nb.NUNA_ERR_TOO_LARGE
+        assert status(name, hidden=(1 << 30) + 1) == nb.NUNA_ERR_TOO_LARGE
     allowed = nb.NUNA_LAUNCH_PDL | (nb.NUNA_GRAD_ACCUMULATE if name in ("nuna_layernorm_backward", "nuna_embedding_backward") else 0)
     for bit in range(32):
         if not (1 << bit) & allowed:
@@ -105,6 +106,7 @@ def test_what_only_one_operator_refuses():
     assert status("nuna_layernorm_backward", workspace_bytes=need - 1) == nb.NUNA_ERR_INVALID_ARG
     assert status("nuna_layernorm_backward", workspace=None) == nb.NUNA_ERR_INVALID_ARG
     need = nb.nuna_embedding_workspace(4, 64, 16)
+    assert status("nuna_embedding_backward", workspace=OPS["nuna_embedding_backward"]["workspace"] + 16) == nb.NUNA_ERR_ALIGNMENT    # 32 bytes a store
     assert status("nuna_embedding_backward", workspace_bytes=need - 1) == nb.NUNA_ERR_INVALID_ARG
     assert status("nuna_embedding_backward", workspace=None) == nb.NUNA_ERR_INVALID_ARG
     assert status("nuna_embedding_backward", grad_dtype=F16) == nb.NUNA_ERR_UNSUPPORTED_DTYPE

@@ -55,6 +55,13 @@ __device__ __forceinline__ float quotient(float sum, float count, float inverse)
     return isfinite(q) ? better : q;
 }
 
+// A thread's packs are 32 apart, a warp's consecutive: the addresses of a row's packs differ by constants.
+__device__ __forceinline__ unsigned first_pack(unsigned lane, unsigned packs) { return lane / 32u * 32u * packs + lane % 32u; }
+template <int DT, bool kVec>
+__device__ __forceinline__ void* pack_at(void* row, unsigned first) { return static_cast<char*>(row) + (size_t)first * (kVec ? 16 : Elem<DT>::kBytes); }
+template <int DT, bool kVec>
+__device__ __forceinline__ const void* pack_at(const void* row, unsigned first) { return static_cast<const char*>(row) + (size_t)first * (kVec ? 16 : Elem<DT>::kBytes); }
+
 // The rows that a group takes, one after the other, fetched ahead of their use.  Vectors go through shared memory by
 // asynchronous copies: a thread fetches, kDepth rows ahead, just the vectors that it will use, so it waits for its own copies
 // only, and what is in flight holds no registers.  Single elements are loaded into registers, a row ahead where there are
@@ -64,13 +71,13 @@ struct RowFetch {
     const void* from[kStreams];
     size_t stride[kStreams];
     bool given[kStreams];
-    unsigned rows, packs, group, lane;
+    unsigned rows, first, packs;                                     // the thread's first pack, and how many there are from it on
     uint32_t slots;                                                  // this thread's part of the shared memory: one slot per fetch
     Pack<DT, kVec> next[kVec ? 1 : kStreams][kVec ? 1 : kPacks];
 
     static constexpr unsigned kSlots = kVec ? kDepth * kStreams * kPacks : 0;       // 16 bytes each, per thread
 
-    __device__ __forceinline__ uint32_t slot(unsigned stage, int s, int k) const { return slots + ((stage * kStreams + s) * kPacks + k) * blockDim.x * 16u; }
+    __device__ __forceinline__ uint32_t slot(unsigned stage, int s, int k) const { return slots + ((stage * kStreams + s) * kPacks + k) * 512u; }
 
     // Starts fetching `row` as the stage-th of the ring.
     __device__ __forceinline__ void start(unsigned long long row, unsigned stage)
@@ -78,13 +85,12 @@ struct RowFetch {
 #pragma unroll
         for (int s = 0; s < kStreams; ++s) {
             if (!given[s]) continue;
-            const void* at = row_at(from[s], (size_t)row, stride[s]);
+            const void* at = pack_at<DT, kVec>(row_at(from[s], (size_t)row, stride[s]), first);
 #pragma unroll
             for (int k = 0; k < kPacks; ++k) {
-                const unsigned i = lane + k * group;
-                if (row < rows && i < packs) {
-                    if constexpr (kVec) copy_async(slot(stage, s, k), static_cast<const uint4*>(at) + i);
-                    else next[s][k] = load_pack<DT, kVec>(at, i);
+                if (row < rows && k * 32u < packs) {
+                    if constexpr (kVec) copy_async(slot(stage, s, k), static_cast<const uint4*>(at) + k * 32);
+                    else next[s][k] = load_pack<DT, kVec>(at, k * 32);
                 }
             }
         }
@@ -130,7 +136,7 @@ struct KeptParams {
 };
 
 // Most threads of a block, and rows that are fetched ahead of the one in work.
-__host__ __device__ constexpr int norm_threads(int packs, bool vec) { return vec && packs == 4 ? 512 : 1024; }
+__host__ __device__ constexpr int norm_threads(int packs, bool vec) { return vec && packs > 1 ? 512 : 1024; }
 __host__ __device__ constexpr int norm_depth(int packs, bool vec) { return !vec ? 2 : packs == 4 ? 2 : 3; }
 
 template <int DT, int PT, int kPacks, bool kVec>
@@ -141,10 +147,11 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
     __shared__ float red[2][32];
     extern __shared__ uint4 ring[];
     const unsigned warps = a.group / 32u, g = threadIdx.x / a.group, lane = threadIdx.x % a.group, groups = blockDim.x / a.group;
+    const unsigned first = first_pack(lane, kPacks), packs = a.packs > first ? a.packs - first : 0u;
     const unsigned long long step = (unsigned long long)gridDim.x * groups;
     unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
     RowFetch<DT, kPacks, kVec, 2, kDepth> fetch = {{a.x, a.residual}, {a.x_stride, a.residual_stride}, {true, a.residual != nullptr},
-                                                   a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
+                                                   a.rows, first, packs, smem_u32(ring + threadIdx.x / 32u * 32u * RowFetch<DT, kPacks, kVec, 2, kDepth>::kSlots + threadIdx.x % 32u), {}};
     pdl_begin(a.rows <= step);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
@@ -153,7 +160,7 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
     KeptParams<PT, E, kPacks, (kVec && kPacks <= 2)> w, b;
 #pragma unroll
     for (int k = 0; k < kPacks; ++k) {
-        const unsigned i = lane + k * a.group;
+        const unsigned i = first + k * 32u;
         w.put(k, load_params<PT, E>(i < a.packs ? a.weight : nullptr, i, kOne<PT>));
         b.put(k, load_params<PT, E>(i < a.packs ? a.bias : nullptr, i, 0u));
     }
@@ -165,18 +172,17 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
             fetch.start(row + (kDepth - 1) * step, stage == 0u ? kDepth - 1 : stage - 1u);
             copy_wait<kDepth - 1>();
         }
-        void* to_sum = row_at(a.summed, (size_t)row, a.summed_stride);
+        void* to_sum = pack_at<DT, kVec>(row_at(a.summed, (size_t)row, a.summed_stride), first);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = lane + k * a.group;
 #pragma unroll
             for (int e = 0; e < P; ++e) f[k][e] = all<V>(0.0f);
-            if (live && i < a.packs) {
+            if (live && k * 32u < packs) {
                 unpack<DT, kVec>(f[k], fetch.take(stage, 0, k));
                 if (a.residual) {
                     add_pack<DT, kVec>(f[k], fetch.take(stage, 1, k));
                     const Pack<DT, kVec> s = pack<DT, kVec>(f[k]);
-                    store_pack<DT, kVec>(to_sum, i, s);
+                    store_pack<DT, kVec>(to_sum, k * 32, s);
                     unpack<DT, kVec>(f[k], s);                       // the norm is that of the stored row
                 }
             }
@@ -194,7 +200,7 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
         part = all<V>(0.0f);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k)
-            if (lane + k * a.group < a.packs)
+            if (k * 32u < packs)
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
                     f[k][e] = f[k][e] + all<V>(-mean);
@@ -208,17 +214,16 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        void* to = row_at(a.y, (size_t)row, a.y_stride);
+        void* to = pack_at<DT, kVec>(row_at(a.y, (size_t)row, a.y_stride), first);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = lane + k * a.group;
-            if (live && i < a.packs) {
+            if (live && k * 32u < packs) {
                 V wf[P], bf[P];
                 w.get(wf, k);
                 b.get(bf, k);
 #pragma unroll
                 for (int e = 0; e < P; ++e) f[k][e] = mad(f[k][e] * all<V>(rstd), wf[e], bf[e]);
-                store_pack<DT, kVec>(to, i, pack<DT, kVec>(f[k]));
+                store_pack<DT, kVec>(to, k * 32, pack<DT, kVec>(f[k]));
             }
         }
         stage = stage + 1u == kDepth ? 0u : stage + 1u;
@@ -301,10 +306,11 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
     __shared__ float red[2][64];
     extern __shared__ uint4 ring[];                                  // in the end, the groups' shares: [groups - 1][2][kPacks * group * E]
     const unsigned warps = a.group / 32u, g = threadIdx.x / a.group, lane = threadIdx.x % a.group, groups = blockDim.x / a.group;
+    const unsigned first = first_pack(lane, kPacks), packs = a.packs > first ? a.packs - first : 0u;
     const unsigned long long step = (unsigned long long)gridDim.x * groups;
     unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
     RowFetch<DT, kPacks, kVec, 3, kDepth> fetch = {{a.x, a.dy, a.dsummed}, {a.x_stride, a.dy_stride, a.dsummed_stride}, {true, true, a.dsummed != nullptr},
-                                                   a.rows, a.packs, a.group, lane, smem_u32(ring + threadIdx.x), {}};
+                                                   a.rows, first, packs, smem_u32(ring + threadIdx.x / 32u * 32u * RowFetch<DT, kPacks, kVec, 3, kDepth>::kSlots + threadIdx.x % 32u), {}};
     pdl_begin(a.rows <= step);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) fetch.start(row + d * step, d);
@@ -314,7 +320,7 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
     KeptParams<PT, E, kPacks, false> w;
 #pragma unroll
     for (int k = 0; k < kPacks; ++k) {
-        const unsigned i = lane + k * a.group;
+        const unsigned i = first + k * 32u;
         w.put(k, load_params<PT, E>(i < a.packs ? a.weight : nullptr, i, kOne<PT>));
 #pragma unroll
         for (int e = 0; e < P; ++e) dw[k][e] = db[k][e] = all<V>(0.0f);
@@ -347,8 +353,7 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
         V c0s = all<V>(0.0f), c1s = all<V>(0.0f);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = lane + k * a.group;
-            if (live && i < a.packs) {
+            if (live && k * 32u < packs) {
                 V dy[P];
                 V (&x)[P] = xh[kKeep ? k : 0];
                 V (&g)[P] = gy[kKeep ? k : 0];
@@ -369,11 +374,10 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
         group_sum<2>(c, warps, g, red[turn]);
         turn ^= 1u;
         const V c0 = all<V>(-c[0] * a.inverse), c1 = all<V>(-c[1] * a.inverse);
-        void* to = row_at(a.dx, (size_t)row, a.dx_stride);
+        void* to = pack_at<DT, kVec>(row_at(a.dx, (size_t)row, a.dx_stride), first);
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
-            const unsigned i = lane + k * a.group;
-            if (live && i < a.packs) {
+            if (live && k * 32u < packs) {
                 V (&s)[P] = r[kDepth == 2 && !kVec ? k : 0];
                 V (&x)[P] = xh[kKeep ? k : 0];
                 V (&g)[P] = gy[kKeep ? k : 0];
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
                 }
 #pragma unroll
                 for (int e = 0; e < P; ++e) s[e] = mad(all<V>(rstd), mad(x[e], c1, g[e] + c0), s[e]);
-                store_pack<DT, kVec>(to, i, pack<DT, kVec>(s));
+                store_pack<DT, kVec>(to, k * 32, pack<DT, kVec>(s));
             }
         }
         stage = stage + 1u == kDepth ? 0u : stage + 1u;
@@ -424,7 +428,7 @@ __global__ void __launch_bounds__(norm_grad_threads(kVec)) k_norm_backward(const
             float* share = a.part + (size_t)blockIdx.x * 2u * a.part_stride;
 #pragma unroll
             for (int k = 0; k < kPacks; ++k) {
-                const unsigned i = lane + k * a.group;
+                const unsigned i = first + k * 32u;
                 if (i < a.packs) {
                     if constexpr (E % 4 == 0) {
 #pragma unroll

@@ -141,18 +141,22 @@ __device__ __forceinline__ void pdl_begin(bool brief = true)
     pdl_wait();
 }
 
-// A pack is what a thread moves at once: a 16-byte vector, or (rows of any length and alignment) one element.
-template <int DT, bool kVec> struct Pack {
-    static constexpr int kElems = kVec ? Elem<DT>::kElems : 1;
-    static constexpr int kWords = kVec ? 4 : 1;
+// A pack is what a thread moves at once: a 16-byte vector, or (rows of any length and alignment) one element, or two elements
+// that need not be neighbours, each in a word of its own, for arithmetic in pairs.  Where only the first two are meant, a bool
+// says which.
+constexpr int kElement = 0, kVector = 1, kPair = 2;
+template <int DT, int kForm> struct Pack {
+    static constexpr int kElems = kForm == kVector ? Elem<DT>::kElems : kForm == kPair ? 2 : 1;
+    static constexpr int kWords = kForm == kVector ? 4 : kElems;
     uint32_t w[kWords];
 };
 
-template <int DT, bool kVec>
-__device__ __forceinline__ Pack<DT, kVec> load_pack(const void* row, size_t i)
+template <int DT, int kForm>
+__device__ __forceinline__ Pack<DT, kForm> load_pack(const void* row, size_t i)
 {
-    Pack<DT, kVec> p;
-    if constexpr (kVec) {
+    static_assert(kForm != kPair);
+    Pack<DT, kForm> p;
+    if constexpr (kForm == kVector) {
         const uint4 v = ld_src(static_cast<const uint4*>(row) + i);
         p.w[0] = v.x, p.w[1] = v.y, p.w[2] = v.z, p.w[3] = v.w;
     } else if constexpr (DT == kF32) {
@@ -164,10 +168,11 @@ __device__ __forceinline__ Pack<DT, kVec> load_pack(const void* row, size_t i)
 }
 
 // kStream: written once and not read again soon (evict-first).
-template <int DT, bool kVec, bool kStream = false>
-__device__ __forceinline__ void store_pack(void* row, size_t i, const Pack<DT, kVec>& p)
+template <int DT, int kForm, bool kStream = false>
+__device__ __forceinline__ void store_pack(void* row, size_t i, const Pack<DT, kForm>& p)
 {
-    if constexpr (kVec) {
+    static_assert(kForm != kPair);
+    if constexpr (kForm == kVector) {
         const uint4 v = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
         if (kStream) st_stream(static_cast<uint4*>(row) + i, v);
         else         st_dst(static_cast<uint4*>(row) + i, v);
@@ -186,29 +191,33 @@ __device__ __forceinline__ void store8(float* p, const float (&f)[8])
                  :: "l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
 }
 
-template <int DT, bool kVec>
-__device__ __forceinline__ void unpack(float (&f)[Pack<DT, kVec>::kElems], const Pack<DT, kVec>& p)
+template <int DT, int kForm>
+__device__ __forceinline__ void unpack(float (&f)[Pack<DT, kForm>::kElems], const Pack<DT, kForm>& p)
 {
     if constexpr (DT == kF32) {
 #pragma unroll
-        for (int i = 0; i < Pack<DT, kVec>::kElems; ++i) f[i] = __uint_as_float(p.w[i]);
-    } else if constexpr (kVec) {
+        for (int i = 0; i < Pack<DT, kForm>::kElems; ++i) f[i] = __uint_as_float(p.w[i]);
+    } else if constexpr (kForm == kVector) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) widen_word<DT>(f[2 * i], f[2 * i + 1], p.w[i]);
     } else {
         float unused;
-        widen_word<DT>(f[0], unused, p.w[0]);
+#pragma unroll
+        for (int i = 0; i < Pack<DT, kForm>::kElems; ++i) widen_word<DT>(f[i], unused, p.w[i]);
     }
 }
 
-template <int DT, bool kVec>
-__device__ __forceinline__ Pack<DT, kVec> pack(const float (&f)[Pack<DT, kVec>::kElems])
+template <int DT, int kForm>
+__device__ __forceinline__ Pack<DT, kForm> pack(const float (&f)[Pack<DT, kForm>::kElems])
 {
-    Pack<DT, kVec> p;
+    Pack<DT, kForm> p;
     if constexpr (DT == kF32) {
 #pragma unroll
-        for (int i = 0; i < Pack<DT, kVec>::kElems; ++i) p.w[i] = __float_as_uint(f[i]);
-    } else if constexpr (kVec) {
+        for (int i = 0; i < Pack<DT, kForm>::kElems; ++i) p.w[i] = __float_as_uint(f[i]);
+    } else if constexpr (kForm == kPair) {
+        const uint32_t both = pack2<DT>(f[0], f[1]);
+        p.w[0] = both & 0xFFFFu, p.w[1] = both >> 16;
+    } else if constexpr (kForm == kVector) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) p.w[i] = pack2<DT>(f[2 * i], f[2 * i + 1]);
     } else {
@@ -425,7 +434,7 @@ __device__ __forceinline__ Two mad(Two a, Two b, Two c)
 __device__ __forceinline__ float mad(float a, float b, float c) { return fmaf(a, b, c); }
 
 // What a pack's arithmetic is done in: pairs, or for a single element a float.
-template <bool kVec> using Lanes = std::conditional_t<kVec, Two, float>;
+template <int DT, int kForm> using Lanes = std::conditional_t<(Pack<DT, kForm>::kElems > 1), Two, float>;
 template <typename V> __device__ __forceinline__ V all(float v);
 template <> __device__ __forceinline__ Two all<Two>(float v) { return {v, v}; }
 template <> __device__ __forceinline__ float all<float>(float v) { return v; }
@@ -434,38 +443,39 @@ __device__ __forceinline__ float total(float v) { return v; }
 __device__ __forceinline__ float& half(Two& v, int i) { return i % 2 ? v.y : v.x; }
 __device__ __forceinline__ float& half(float& v, int) { return v; }
 
-template <int DT, bool kVec> constexpr int kLanes = (Pack<DT, kVec>::kElems + 1) / 2;
+template <int DT, int kForm> constexpr int kLanes = (Pack<DT, kForm>::kElems + 1) / 2;
 
-template <int DT, bool kVec>
-__device__ __forceinline__ void unpack(Two (&f)[kLanes<DT, kVec>], const Pack<DT, kVec>& p)
+template <int DT, int kForm>
+__device__ __forceinline__ void unpack(Two (&f)[kLanes<DT, kForm>], const Pack<DT, kForm>& p)
 {
-    float v[Pack<DT, kVec>::kElems];
-    unpack<DT, kVec>(v, p);
+    float v[Pack<DT, kForm>::kElems];
+    unpack<DT, kForm>(v, p);
 #pragma unroll
-    for (int i = 0; i < kLanes<DT, kVec>; ++i) f[i] = {v[2 * i], v[2 * i + 1]};
+    for (int i = 0; i < kLanes<DT, kForm>; ++i) f[i] = {v[2 * i], v[2 * i + 1]};
 }
-template <int DT, bool kVec>
-__device__ __forceinline__ Pack<DT, kVec> pack(const Two (&f)[kLanes<DT, kVec>])
+template <int DT, int kForm>
+__device__ __forceinline__ Pack<DT, kForm> pack(const Two (&f)[kLanes<DT, kForm>])
 {
-    float v[Pack<DT, kVec>::kElems];
+    float v[Pack<DT, kForm>::kElems];
 #pragma unroll
-    for (int i = 0; i < kLanes<DT, kVec>; ++i) v[2 * i] = f[i].x, v[2 * i + 1] = f[i].y;
-    return pack<DT, kVec>(v);
+    for (int i = 0; i < kLanes<DT, kForm>; ++i) v[2 * i] = f[i].x, v[2 * i + 1] = f[i].y;
+    return pack<DT, kForm>(v);
 }
 // f += the pack's elements: one instruction for a 16-bit element, none for widening it.
-template <int DT, bool kVec>
-__device__ __forceinline__ void add_pack(Lanes<kVec> (&f)[kLanes<DT, kVec>], const Pack<DT, kVec>& p)
+template <int DT, int kForm>
+__device__ __forceinline__ void add_pack(Lanes<DT, kForm> (&f)[kLanes<DT, kForm>], const Pack<DT, kForm>& p)
 {
     if constexpr (DT == kF32) {
-        Lanes<kVec> r[kLanes<DT, kVec>];
-        unpack<DT, kVec>(r, p);
+        Lanes<DT, kForm> r[kLanes<DT, kForm>];
+        unpack<DT, kForm>(r, p);
 #pragma unroll
-        for (int i = 0; i < kLanes<DT, kVec>; ++i) f[i] = f[i] + r[i];
+        for (int i = 0; i < kLanes<DT, kForm>; ++i) f[i] = f[i] + r[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < kLanes<DT, kVec>; ++i) {
+        for (int i = 0; i < kLanes<DT, kForm>; ++i) {
             half(f[i], 0) = add_narrow<DT>(half(f[i], 0), (uint16_t)p.w[i]);
-            if (kVec) half(f[i], 1) = add_narrow<DT>(half(f[i], 1), (uint16_t)(p.w[i] >> 16));
+            if constexpr (kForm == kVector) half(f[i], 1) = add_narrow<DT>(half(f[i], 1), (uint16_t)(p.w[i] >> 16));
+            if constexpr (kForm == kPair)   half(f[i], 1) = add_narrow<DT>(half(f[i], 1), (uint16_t)p.w[i + 1]);
         }
     }
 }

@@ -1,7 +1,7 @@
 // Embedding lookup over a slice of the vocabulary, and its gradient by sorted tokens.
 //
 // Both are rows moved by an index: what bounds them is the memory, and for a few tokens the two dependent reads, id and row.
-// The gradient sorts the tokens by id (k_embedding_sort), so that the tokens of a table row are a run of consecutive positions,
+// The gradient sorts the tokens by id (k_embedding_sort: a few by comparing all of them, more digit by digit), so that the tokens of a table row are a run of consecutive positions,
 // in the tokens' order; then every table row is written once, by the threads that have added its run in registers.  Runs of
 // more than kRunPart tokens are cut at the positions that are multiples of kRunPart, their parts added by blocks of their own
 // and joined in order, so that one frequent id does not keep one block busy.
@@ -90,10 +90,62 @@ struct SortArgs {
     long long vocab_start;
     unsigned tokens, vocab_rows, passes, bits;                       // bits of a digit
     unsigned sorters;                                                // blocks that sort; the others zero the table
+    unsigned per, slices;                                            // by rank: a block's tokens, threads that count for one; 0: by digits
     bool clear;                                                      // rows without a token get end = 0
     uint4* zero;
     unsigned long long zero_vectors;
+    uint16_t *head, *tail;                                           // what the table has in front of those vectors and behind them
+    unsigned head_halves, tail_halves;
 };
+
+// The place of each of a few tokens is the number of tokens that belong before it: a block has all tokens' rows in its shared
+// memory, and `slices` threads compare a share of them each with the row of one of its `per` tokens.  Returns how many tokens
+// have a row; keys, [tokens + 3] and [tokens] behind, holds their rows and, if one block sorts, those in order.
+template <typename RowAt>
+__device__ __forceinline__ unsigned rank_tokens(const SortArgs& a, unsigned* keys, uint2* to, RowAt row_at_token)
+{
+    const unsigned vectors = (a.tokens + 3u) / 4u;
+    unsigned *sorted = keys + vectors * 4u, *part = sorted + a.tokens, n = 0;
+    for (unsigned base = 0; base < vectors * 4u; base += blockDim.x) {
+        const unsigned j = base + threadIdx.x, key = j < a.tokens ? row_at_token(j) : kNoDigit;
+        if (j < vectors * 4u) keys[j] = key;
+        n += __syncthreads_count(key != kNoDigit);
+    }
+    const unsigned slice = threadIdx.x / a.per, mine = threadIdx.x - slice * a.per, i = blockIdx.x * a.per + mine;
+    const unsigned key = i < a.tokens ? keys[i] : kNoDigit;
+    if (slice < a.slices) {
+        const unsigned each = (vectors + a.slices - 1u) / a.slices, from = slice * each, to_vector = from + each < vectors ? from + each : vectors;
+        const unsigned own = (i - threadIdx.x % 32u) / 4u;           // the first of the eight vectors that hold this warp's tokens
+        const uint4* all = reinterpret_cast<const uint4*>(keys);
+        unsigned count = 0, j = from;
+#pragma unroll 4
+        for (; j < to_vector && j < own; ++j) {                      // earlier tokens come first among equals
+            const uint4 k = all[j];
+            count += (unsigned)(k.x <= key) + (unsigned)(k.y <= key) + (unsigned)(k.z <= key) + (unsigned)(k.w <= key);
+        }
+        for (; j < to_vector && j < own + 8u; ++j) {
+            const uint4 k = all[j];
+            const unsigned t = j * 4u;
+            count += (unsigned)(k.x < key || (k.x == key && t < i)) + (unsigned)(k.y < key || (k.y == key && t + 1u < i)) +
+                     (unsigned)(k.z < key || (k.z == key && t + 2u < i)) + (unsigned)(k.w < key || (k.w == key && t + 3u < i));
+        }
+#pragma unroll 4
+        for (; j < to_vector; ++j) {
+            const uint4 k = all[j];
+            count += (unsigned)(k.x < key) + (unsigned)(k.y < key) + (unsigned)(k.z < key) + (unsigned)(k.w < key);
+        }
+        part[threadIdx.x] = count;
+    }
+    __syncthreads();
+    if (slice == 0u && key != kNoDigit) {
+        unsigned rank = 0;
+        for (unsigned s = 0; s < a.slices; ++s) rank += part[s * a.per + mine];
+        to[rank] = make_uint2(i, key);
+        sorted[rank] = key;
+    }
+    sort_sync(a.sorters);
+    return n;
+}
 
 // items[passes & 1 ^ 1]: the tokens with a row in the slice, by row and then by token; begin / end: each row's run; count: how
 // many tokens that is, and how many runs are cut; cut: where those begin, in no order (each of them is joined by itself).
@@ -114,6 +166,8 @@ __global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> 
     const unsigned bins = 1u << a.bits, threads = a.sorters * blockDim.x, thread = blockIdx.x * blockDim.x + threadIdx.x;
     const Id* ids = static_cast<const Id*>(a.ids);
     if (thread == 0u) a.count[1] = 0u;                               // like `end`, before the first pass
+    if (thread < a.head_halves) a.head[thread] = 0;
+    if (thread < a.tail_halves) a.tail[thread] = 0;
     if (a.clear)                                                     // whose barriers order it
         // 16 bytes a store; the rest of the last vector is the workspace's padding
         for (unsigned long long v = thread; v * 4u < a.vocab_rows; v += threads) reinterpret_cast<uint4*>(a.end)[v] = make_uint4(0u, 0u, 0u, 0u);
@@ -122,28 +176,33 @@ __global__ void __launch_bounds__(1024) k_embedding_sort(const Padded<SortArgs> 
         return id >= a.vocab_start && from < a.vocab_rows ? (unsigned)from : kNoDigit;
     };
     uint2 *to = a.items[0], *from = a.items[1];
-    const unsigned n = sort_pass<long long>(a.sorters, a.tokens, bins, smem, nullptr,
-        [&](unsigned i) { return load_id(ids + i); },
-        [&](long long id) {
-            const unsigned row = row_of(id);
-            return row == kNoDigit ? kNoDigit : row & (bins - 1u);
-        },
-        [&](unsigned i, long long id, unsigned d, unsigned first, unsigned rank) {
-            if (d != kNoDigit) to[first + rank] = make_uint2(i, row_of(id));
-        });
-    for (unsigned pass = 1; pass < a.passes; ++pass) {
-        uint2* last = to;
-        to = from, from = last;
-        sort_pass<uint2>(a.sorters, n, bins, smem, nullptr, [&](unsigned i) { return load_shared_by_cluster(from + i); },
-            [&](uint2 item) { return (item.y >> (pass * a.bits)) & (bins - 1u); },
-            [&](unsigned, uint2 item, unsigned, unsigned first, unsigned rank) { to[first + rank] = item; });
+    unsigned n;
+    if (a.per) {
+        n = rank_tokens(a, smem, to, [&](unsigned i) { return row_of(load_id(ids + i)); });
+    } else {
+        n = sort_pass<long long>(a.sorters, a.tokens, bins, smem, nullptr,
+            [&](unsigned i) { return load_id(ids + i); },
+            [&](long long id) {
+                const unsigned row = row_of(id);
+                return row == kNoDigit ? kNoDigit : row & (bins - 1u);
+            },
+            [&](unsigned i, long long id, unsigned d, unsigned first, unsigned rank) {
+                if (d != kNoDigit) to[first + rank] = make_uint2(i, row_of(id));
+            });
+        for (unsigned pass = 1; pass < a.passes; ++pass) {
+            uint2* last = to;
+            to = from, from = last;
+            sort_pass<uint2>(a.sorters, n, bins, smem, nullptr, [&](unsigned i) { return load_shared_by_cluster(from + i); },
+                [&](uint2 item) { return (item.y >> (pass * a.bits)) & (bins - 1u); },
+                [&](unsigned, uint2 item, unsigned, unsigned first, unsigned rank) { to[first + rank] = item; });
+        }
     }
+    const auto row_in_order = [&](size_t p) { return a.per && a.sorters == 1u ? smem[(a.tokens + 3u) / 4u * 4u + p] : load_shared_by_cluster(to + p).y; };
     for (unsigned long long p = thread; p < n; p += threads) {
-        const unsigned v = load_shared_by_cluster(to + p).y;
-        const unsigned left = p > 0 ? load_shared_by_cluster(to + p - 1).y : kNoDigit, right = p + 1 < n ? load_shared_by_cluster(to + p + 1).y : kNoDigit;
+        const unsigned v = row_in_order(p), left = p > 0 ? row_in_order(p - 1) : kNoDigit, right = p + 1 < n ? row_in_order(p + 1) : kNoDigit;
         if (left != v) a.begin[v] = (unsigned)p;
         if (right != v) a.end[v] = (unsigned)p + 1u;
-        if (left != v && p + kRunPart < n && load_shared_by_cluster(to + p + kRunPart).y == v) a.cut[atomicAdd(a.count + 1, 1u)] = (unsigned)p;
+        if (left != v && p + kRunPart < n && row_in_order(p + kRunPart) == v) a.cut[atomicAdd(a.count + 1, 1u)] = (unsigned)p;
     }
     if (thread == 0u) a.count[0] = n;
     pdl_trigger();
@@ -455,6 +514,11 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
     return with_dtype(n.dtype, [&](auto dt) { return n.id_bytes == 8 ? typed((long long)0, dt) : typed(0, dt); });
 }
 
+// Tokens that are placed by rank, in one block and at all.  Comparisons grow with the square, but there is one pass and one wait
+// instead of a dozen a digit (the whole gradient, to 32768 rows: 32 tokens 9.6 -> 5.3 us, 128 10.9 -> 6.9, 400 16.3 -> 9.4, 1024 16.6 ->
+// 13.4; 2048 18.8 by digits against 21.6; in one block and in eight 64 tokens 6.1 both, 128 6.9 | 7.2, 256 8.6 | 8.0).
+constexpr size_t kRankAlone = 128, kRankTokens = 1024;
+
 constexpr size_t kZeroBytes = 384 << 10;                             // that a block zeroes, about: 7.2 TB/s; with 113 KB and 3.6 MB 7.0 and 6.5
 
 static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* stream)
@@ -472,7 +536,7 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     // sort outlasts the stores (3 ns a token in one block).
     const bool vec = VectorRows{true}.rows(n.dout, n.hidden, n.dout_stride, e).rows(n.dtable, n.hidden, n.dtable_stride, ge).ok;
     const bool whole = n.dtable_stride == 0 || n.dtable_stride == n.hidden;
-    const bool zero_first = !accumulate && vec && whole && n.tokens && n.tokens * 4 <= n.vocab_rows && n.tokens <= 16384 &&
+    const bool zero_first = !accumulate && whole && n.tokens && n.tokens * 4 <= n.vocab_rows && n.tokens <= 16384 &&
                             n.vocab_rows * n.hidden * ge >= n.tokens * (24 << 10);
     s.clear = !accumulate && !zero_first;
     for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint2*>(words(w.items[i]));
@@ -483,13 +547,24 @@ static int table_gradient(const nuna_embedding_grad_t& n, unsigned flags, void* 
     s.bits = (bits + s.passes - 1u) / s.passes;
     if (n.tokens) {
         Shape sort = sort_shape(n.tokens, 1u << s.bits);
+        if (n.tokens <= (zero_first ? kRankTokens / 2 : kRankTokens)) {
+            s.passes = 1;
+            sort.grid = sort.cluster = n.tokens <= kRankAlone || zero_first ? 1 : 8;
+            s.per = (unsigned)((n.tokens + sort.grid - 1) / sort.grid + 31) / 32 * 32;
+            s.slices = std::max(1u, std::min(1024u / s.per, (unsigned)n.tokens / 16u));
+            sort.block = std::max(s.per * s.slices, zero_first ? 1024u : 128u);
+            sort.smem = (unsigned)(n.tokens * 2 + 3 + sort.block) * 4;
+        }
         s.sorters = sort.grid;
         if (zero_first) {
-            s.zero = static_cast<uint4*>(n.dtable), s.zero_vectors = n.vocab_rows * n.hidden * ge / 16;
+            const uintptr_t begin = (uintptr_t)n.dtable, end = begin + n.vocab_rows * n.hidden * ge, from = std::min(end, (begin + 15) / 16 * 16);
+            s.zero = reinterpret_cast<uint4*>(from), s.zero_vectors = (end - from) / 16;
+            s.head = static_cast<uint16_t*>(n.dtable), s.head_halves = (unsigned)(from - begin) / 2;
+            s.tail = reinterpret_cast<uint16_t*>(from + s.zero_vectors * 16), s.tail_halves = (unsigned)(end - from) % 16 / 2;
             s.sorters = 1;                                           // the sort is hidden: a cluster would only leave SMs without a block
             const size_t wave = (kSms - 1) * kZeroBytes;             // one of these blocks is resident on an SM
             const unsigned blocks = (kSms - 1) * (unsigned)std::max<size_t>(1, (n.vocab_rows * n.hidden * ge + wave / 2) / wave);
-            sort = Shape{1 + blocks, kSortMaxWarps * 32u, sort_smem(kSortMaxWarps, 1u << s.bits), 1};
+            sort = Shape{1 + blocks, kSortMaxWarps * 32u, s.per ? sort.smem : sort_smem(kSortMaxWarps, 1u << s.bits), 1};
         }
         constexpr int kMost = sort_smem(kSortMaxWarps, 1024);
         const bool wide = n.id_bytes == 8;

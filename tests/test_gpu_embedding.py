@@ -12,7 +12,9 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 1, 1, 0, 1), (1, 8, 5, 0, 5), (3, 7, 4, 2, 9), (64, 64, 16, 0, 16), (65, 64, 16, 0, 16), (63, 33, 1, 0, 1), (129, 40, 1, 0, 2),
           (1000, 256, 37, 100, 200), (257, 1024, 1000, 0, 1000), (500, 1037, 300, 17, 400), (2500, 520, 3, 0, 3), (300, 8192, 50, 0, 64),
           (8193, 72, 1025, 0, 1025), (20000, 24, 131072, 0, 131072), (70000, 16, 2049, 5, 3000), (37, 16392, 9, 0, 9), (4, 65537, 3, 0, 4),
-          (150000, 8, 40000, 0, 40000), (300, 520, 5000, 100, 6000), (5000, 4096, 30000, 0, 60000), (16390, 40, 70000, 0, 70000)]
+          (150000, 8, 40000, 0, 40000), (300, 520, 5000, 100, 6000), (5000, 4096, 30000, 0, 60000), (16390, 40, 70000, 0, 70000),
+          (100, 1001, 4000, 5, 5000), (128, 24, 77, 3, 90), (513, 1001, 16000, 0, 16000), (512, 72, 300, 0, 300), (1024, 33, 5000, 9, 5100),
+          (1025, 40, 2000, 0, 2000)]
 IDS = {"i32": torch.int32, "i64": torch.int64}
 
 

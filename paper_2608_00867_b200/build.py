@@ -87,7 +87,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     build_native(force, verbose)
     if not force and not is_stale():
         return LIB
-    _compile([os.environ.get("NVCC", "nvcc")] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + sources(), LIB, verbose)
+    _compile([os.environ.get("NVCC", "nvcc"), "--threads", "0"] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + sources(), LIB, verbose)
     return LIB
 
 

@@ -214,6 +214,24 @@ def test_backward_with_gaps_odd_alignment_and_without_options(rows, hidden, dtyp
     run_backward(rows, hidden, dtype, param, accumulate=True, want_bias=False)
 
 
+@pytest.mark.parametrize("dtype,param", PARAMS)
+@pytest.mark.parametrize("hidden", [63, 65, 255, 257, 511, 512, 513, 1023, 1024, 1025, 1537, 4095, 4096, 4097, 6001, 8191, 8192, 8193])
+def test_rows_that_end_at_and_around_a_warps_columns(hidden, dtype, param):
+    for rows in (1, 17):
+        for residual in (False, True):
+            run_forward(rows, hidden, dtype, param, residual=residual, pad=5)
+            run_backward(rows, hidden, dtype, param, dsummed=residual, pad=5)
+    run_forward(400, hidden, dtype, param, residual=True, pad=3, shift=1)                 # more rows than there are SMs: fetched ahead
+    run_backward(400, hidden, dtype, param, dsummed=True, pad=3, shift=1)
+
+
+@pytest.mark.parametrize("dtype,param,hidden", [("bf16", "f32", 8193), ("f16", "f16", 16392), ("f32", "f32", 8200)])
+@pytest.mark.parametrize("rows", [148, 149, 148 * 16, 148 * 16 + 1, 148 * 33 + 5])
+def test_long_rows_in_several_batches(rows, hidden, dtype, param):
+    run_backward(rows, hidden, dtype, param, dsummed=True)
+    run_backward(rows, hidden, dtype, param, accumulate=True, pad=3)
+
+
 @pytest.mark.parametrize("rows,hidden", [(1500, 96), (700, 1001), (333, 8192)])
 def test_the_same_call_gives_the_same_bits(rows, hidden):
     first = run_backward(rows, hidden, "bf16", "f32", dsummed=True)

@@ -222,12 +222,14 @@ __global__ void __launch_bounds__(256) k_expert_combine(const Padded<MoveArgs> a
 }
 
 // A token per group of threads, which goes over the row kPacks pieces a thread at a time; kBatch pairs' products are summed
-// together, and over the group at the end of the row.
-template <int DT, int kPacks, bool kWhole>
-__global__ void __launch_bounds__(256) k_expert_combine_backward(const Padded<MoveArgs> a)
+// together, and over the group at the end of the row.  Pieces of rows that are not whole vectors hold three times the registers:
+// one pair at a time and five blocks on an SM, instead of two pairs in two or three (4096 x 2051 bf16, 8 of 64: 103 against 138 us,
+// 2048 x 2050 f32, 2 of 16: 25 | 39); where all tokens find a place at once with two pairs, two (100 x 2050, 4 of 16: 7.4 against 9.3,
+// 450 x 2051 12.1 | 10.2, 1000 x 333 10.7 | 13.4).
+template <int DT, int kPacks, bool kWhole, int kBatch>
+__global__ void __launch_bounds__(256, kBatch > 1 ? 2 : DT == kF32 ? 4 : 5) k_expert_combine_backward(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
-    constexpr int kBatch = kWhole ? 4 : 2;                           // pairs in flight
     __shared__ float red[2][8][kBatch];
     pdl_begin();
     if (blockIdx.x < a.zero_blocks) {
@@ -337,13 +339,20 @@ static size_t stride_bytes(size_t stride, size_t hidden, int dtype) { return (st
 // Pieces of 16 bytes that a row may be cut into.
 static unsigned pieces(size_t hidden, size_t size, bool whole) { return (unsigned)(whole ? hidden * size / 16 : (hidden + 2 * (16 / size) - 2) / (16 / size)); }
 
+// Threads of a group, at most `most`, for a row in steps of about the same length.
+static unsigned group_of(unsigned packs, int per_thread, unsigned most)
+{
+    const unsigned threads = (packs + per_thread - 1) / per_thread, steps = std::max(1u, (threads + most - 1) / most);
+    return std::max(32u, ((threads + steps - 1) / steps + 31u) / 32u * 32u);
+}
+
 // Launches a row mover with kPacks pieces a thread in groups of at most `most` threads, which take chunks of a row, or (`whole`)
 // a row in several steps.
 template <typename Kernel>
 static int move_rows(Kernel kernel, MoveArgs& a, size_t tokens, int per_thread, unsigned most, bool whole, unsigned flags, void* stream)
 {
     const unsigned threads = (a.packs + per_thread - 1) / per_thread, steps = std::max(1u, (threads + most - 1) / most);
-    a.group = std::max(32u, ((threads + steps - 1) / steps + 31u) / 32u * 32u);          // steps of about the same length
+    a.group = group_of(a.packs, per_thread, most);
     a.chunks = whole ? 1u : steps;
     const unsigned groups = std::max(1u, 256u / a.group);
     const unsigned long long units = (unsigned long long)tokens * a.chunks;
@@ -385,9 +394,10 @@ static int combine(const nuna_expert_combine_t& n, unsigned flags, void* stream)
     a.topk = (unsigned)n.topk, a.rows = (unsigned)n.rows, a.packs = pieces(n.hidden, e, vec), a.hidden = (unsigned)n.hidden, a.tokens = (unsigned)n.tokens;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine<DT, 2, false>, a, n.tokens, 2, 256, false, flags, stream);
-        return (unsigned long long)n.tokens * a.packs <= 2ull * kSms * 512ull
-                   ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, 256, false, flags, stream)
+        const bool few = (unsigned long long)n.tokens * a.packs <= 2ull * kSms * 512ull;       // too few for two pieces a thread
+        if (!vec) return few ? move_rows(k_expert_combine<DT, 1, false>, a, n.tokens, 1, 256, false, flags, stream)
+                             : move_rows(k_expert_combine<DT, 2, false>, a, n.tokens, 2, 256, false, flags, stream);
+        return few ? move_rows(k_expert_combine<DT, 1, true>, a, n.tokens, 1, 256, false, flags, stream)
                    : move_rows(k_expert_combine<DT, 2, true>, a, n.tokens, 2, 256, false, flags, stream);
     });
 }
@@ -406,8 +416,10 @@ static int combine_backward(const nuna_expert_combine_grad_t& n, unsigned flags,
     const size_t tokens = n.topk ? n.tokens : 0;
     return with_dtype(n.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if (!vec) return move_rows(k_expert_combine_backward<DT, 1, false>, a, tokens, 1, 256, true, flags, stream);
-        return move_rows(k_expert_combine_backward<DT, 2, true>, a, tokens, 2, 128, true, flags, stream);
+        const bool few = tokens <= kSms * (512u / group_of(a.packs, 1, 256));                 // all at once with two pairs
+        if (!vec) return few ? move_rows(k_expert_combine_backward<DT, 1, false, 2>, a, tokens, 1, 256, true, flags, stream)
+                             : move_rows(k_expert_combine_backward<DT, 1, false, 1>, a, tokens, 1, 256, true, flags, stream);
+        return move_rows(k_expert_combine_backward<DT, 2, true, 4>, a, tokens, 2, 128, true, flags, stream);
     });
 }
 

@@ -509,7 +509,8 @@ static int lookup(const nuna_embedding_t& n, unsigned flags, void* stream)
         };
         const bool few = (unsigned long long)n.tokens * packs <= 4ull * kSms * 512ull;     // too few for every SM to hold more than one a thread
         if (vec) return few ? run(k_embedding_lookup<Id, DT, 1, 1, true>, 1, 1) : run(k_embedding_lookup<Id, DT, 4, 2, true>, 4, 2);
-        return few ? run(k_embedding_lookup<Id, DT, 1, 1, false>, 1, 1) : run(k_embedding_lookup<Id, DT, 4, 1, false>, 4, 1);
+        // (two tokens and two pieces, against four and one: 16384 x 4001 bf16 43.8 | 50.2 us, 20011 x 1037 f32 30.7 | 37.6)
+        return few ? run(k_embedding_lookup<Id, DT, 1, 1, false>, 1, 1) : run(k_embedding_lookup<Id, DT, 2, 2, false>, 2, 2);
     };
     return with_dtype(n.dtype, [&](auto dt) { return n.id_bytes == 8 ? typed((long long)0, dt) : typed(0, dt); });
 }

@@ -106,7 +106,9 @@ template <int DT, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_expert_dispatch(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
-    constexpr int kAhead = kWhole ? 8 : 4;                           // rows of the map that are fetched together
+    // Rows of the map that are fetched together; pieces, also the rows that are written together (1 | 2 | 4: 8192 x 2050 f32, 2 of 16:
+    // 45 | 50 | 74 us, 4096 x 2051 bf16, 8 of 64: 38.8 | 37.6 | 43.8).
+    constexpr int kAhead = kWhole ? 8 : DT == kF32 ? 1 : 2;
     pdl_begin();
     if (blockIdx.x < a.zero_blocks) {
         zero_empty_rows<DT, kWhole>(a);
@@ -165,7 +167,9 @@ template <int DT, int kPacks, bool kWhole>
 __global__ void __launch_bounds__(256) k_expert_combine(const Padded<MoveArgs> a)
 {
     constexpr int E = Elem<DT>::kElems;
-    constexpr int kAhead = kWhole && kPacks == 1 ? 8 : 4;            // expert rows in flight
+    // Expert rows in flight.  Pieces hold twice the registers of vectors: blocks are worth more than rows ahead in each (one and four:
+    // 8192 x 2050 f32, 2 of 16: 56 and 116 us, 4096 x 2051 bf16, 8 of 64: 46 | 59), but for few tokens, which have the SMs to themselves.
+    constexpr int kAhead = kWhole ? (kPacks == 1 ? 8 : 4) : kPacks == 1 ? 4 : 1;
     pdl_begin();
     const unsigned groups = blockDim.x / a.group, lane = threadIdx.x % a.group;
     const unsigned unit = blockIdx.x * groups + threadIdx.x / a.group;

@@ -98,7 +98,7 @@ def test_sort_of_one_expert_and_of_nobody():
 MOVES = [(1, 1, 1, 1, 1, 0), (1, 8, 64, 8, 8, 0), (5, 2, 8, 3, 5, 0), (32, 8, 4096, 64, 64, 0), (33, 3, 31, 7, 20, 0), (40, 9, 1037, 6, 6, 0),
          (17, 5, 1032, 4, 4, 30), (100, 2, 520, 10, 20, 3), (64, 4, 8192, 16, 16, 0), (9, 3, 16392, 4, 4, 8), (700, 6, 264, 30, 60, 50),
          (3, 17, 100, 40, 40, 0), (3000, 2, 48, 8, 8, 0), (4, 3, 65537, 4, 4, 0),
-         (500, 4, 2051, 16, 16, 0), (1300, 3, 333, 8, 8, 0), (470, 3, 1031, 12, 30, 40)]
+         (500, 4, 2051, 16, 16, 0), (700, 3, 2051, 9, 16, 0), (1300, 3, 333, 8, 8, 0), (470, 3, 1031, 12, 30, 40)]
 
 
 def setup(shape, pads, shift, dtype):

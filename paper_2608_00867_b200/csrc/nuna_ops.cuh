@@ -38,12 +38,14 @@ inline int check_spans(const Spans& s, int twin_a = -1, int twin_b = -1)
     return NUNA_OK;
 }
 
-// Whether every matrix's rows are whole 16-byte vectors at 16-byte addresses.
+// Whether every matrix's rows are whole 16-byte vectors at 16-byte addresses.  A matrix that is not given has no addresses, but
+// its rows' length counts all the same: kernels cut all rows by it (no tokens: a 16-bit dout that need not be there and its
+// binary32 dtable, whose rows of 4 elements are a whole vector, are cut in eights).
 struct VectorRows {
     bool ok;
     VectorRows& rows(const void* at, size_t elems, size_t stride, size_t size)
     {
-        ok = ok && (!at || !(((uintptr_t)at | (stride ? stride : elems) * size | elems * size) & 15u));
+        ok = ok && !((elems * size) & 15u) && (!at || !(((uintptr_t)at | (stride ? stride : elems) * size) & 15u));
         return *this;
     }
 };

@@ -224,6 +224,19 @@ def test_empty_calls_that_write():
                                workspace=torch.empty(nb.nuna_embedding_workspace(5, 24, 0), dtype=torch.uint8, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype,grad", [("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("hidden", [1, 4, 12, 20, 516, 1028, 1540, 2052, 4100, 8196])
+def test_empty_calls_write_every_column(hidden, dtype, grad):
+    """No tokens and no dout: all of the gradient is zeros, where its rows are whole vectors and dout's would not be, too."""
+    for pad in (0, 4):
+        for tokens_of in (None, torch.empty(0, hidden, dtype=DTYPES[dtype][0], device="cuda")):
+            dtable = Rows(9, hidden, DTYPES[grad][0], pad)
+            nb.nuna_embedding_backward(None, tokens_of, dtable.flat, 0, hidden, 9, dtype=DTYPES[dtype][1], grad_dtype=DTYPES[grad][1],
+                                       dtable_stride=dtable.stride)
+            torch.cuda.synchronize()
+            assert bool((dtable.v == 0).all()) and dtable.untouched()
+
+
 def test_rows_beyond_32_bits():
     """A table of more than 2^32 elements: the last row is reached, and its gradient written, at the right place."""
     hidden, rows = 4096, (1 << 20) + 3

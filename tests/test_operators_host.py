@@ -1,6 +1,9 @@
 """Refusals and empty calls of the operators around the collectives: everything that is decided before any CUDA call."""
 import ctypes
 import inspect
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -145,6 +148,21 @@ def test_empty_calls_launch_nothing():
     assert status("nuna_expert_combine", hidden=0) == nb.NUNA_OK
     assert status("nuna_expert_combine_backward", tokens=0, pair_of_row=None) == nb.NUNA_OK
     assert nb.nuna_launch_count() == before
+
+
+@pytest.mark.parametrize("hidden", [1, 4, 12, 516, 8196])
+def test_a_gradient_of_no_tokens_reaches_its_launch(hidden):
+    """Absent rows of a 16-bit dout beside a binary32 table whose own rows are whole vectors.  In a process that sees no GPU, where
+    the launch is refused and the addresses are never used."""
+    code = f"""
+from paper_2608_00867_b200 import binding as nb
+for dtype in (nb.NUNA_BF16, nb.NUNA_F16):
+    st = nb.nuna_embedding_backward(None, None, {BUF[2]}, 0, {hidden}, 9, dtype=dtype, grad_dtype=nb.NUNA_F32, stream=0, check=False)
+    assert st == nb.NUNA_ERR_CUDA, st
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True,
+                          text=True, timeout=300, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""})
+    assert done.returncode == 0, (done.returncode, done.stderr[-2000:])
 
 
 def test_workspaces_of_impossible_sizes():

@@ -171,6 +171,22 @@ def test_zeros_of_no_row_are_not_scaled():
         assert bool((out[1:] == 0).all()) and torch.equal(out[0], torch.full_like(out[0], want)) or want != want and bool(torch.isnan(out[0]).all())
 
 
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("hidden", [1, 24, 37, 1032])
+@pytest.mark.parametrize("scale", [float("inf"), float("-inf"), float("nan"), 0.0, 3.0])
+def test_rows_of_no_token_are_zeros_at_any_scale(scale, hidden, dtype):
+    tdt, code = DTYPES[dtype]
+    for tokens in (3, 3000):
+        ids = torch.tensor([1, 2, -5], device="cuda").repeat(tokens // 3)
+        out = torch.full((tokens, hidden), GUARD, dtype=tdt, device="cuda")
+        nb.nuna_embedding_forward(ids, torch.ones(2, hidden, dtype=tdt, device="cuda"), out, tokens, hidden, 2, scale=scale, dtype=code)
+        assert bool((out[ids != 1] == 0).all())
+        if scale != scale:
+            assert bool(torch.isnan(out[ids == 1]).all())
+        else:
+            assert bool((out[ids == 1] == scale).all())
+
+
 def test_the_first_call_of_a_process_may_be_captured():
     code = """
 import torch

@@ -183,3 +183,51 @@ def test_gaps_that_hold_nan_change_nothing(dtype, pad, shift):
     want, got = run(0, 0), run(pad, shift)
     for n in want:
         assert not bool(torch.isnan(want[n]).any()) and torch.equal(want[n], got[n]), (n, dtype, pad, shift)
+
+
+@pytest.mark.parametrize("flags", [0, nb.NUNA_LAUNCH_PDL])
+@pytest.mark.parametrize("n,vectors", [(2, 40), (4, 148 * 32 + 1), (8, 148 * 96 + 7), (8, 148 * 8 - 1), (3, (7 << 20) // 16)])
+def test_two_shots_with_short_operators_between_them(n, vectors, flags):
+    """Short grids release their successor ahead of their own wait, so a two-shot, which may draw its tickets ahead of its wait, can
+    start while the two-shot before the operator still runs.  A lookup writes what the first two-shot sums, a combine copies each one's
+    result before the next one overwrites it; eager and replayed, in the tagged form and beyond it.  Small integers: exact."""
+    hidden, tokens = 64, 4
+    count, head = 8 * vectors + 8, tokens * hidden
+    gen = generator(n, vectors)
+    ids = torch.tensor([3, 9, 0, 1], device="cuda")
+    src = [[integers(gen, -2, 2, count).bfloat16() for _ in range(n)] for _ in range(2)]
+    tables = [integers(gen, -2, 2, 4, hidden).bfloat16() for _ in range(2)]
+    dst = [torch.zeros(count, dtype=torch.bfloat16, device="cuda") for _ in range(n)]
+    seen = [torch.zeros(tokens, hidden, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    row = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    want = []
+    for i in range(2):
+        looked = torch.where((ids < 4)[:, None], tables[i][ids.clamp(max=3)].float() * 2, torch.zeros(1, device="cuda"))
+        src[i][0][:head] = looked.reshape(-1).bfloat16()
+        want.append(torch.stack([s.float() for s in src[i]]).sum(0).bfloat16())
+    nb.nuna_init(2 * count)
+
+    def look(i):
+        nb.nuna_embedding_forward(ids, tables[i], src[i][0], tokens, hidden, 4, scale=2.0, flags=flags)
+
+    def reduce(i):
+        nb.nuna_allreduce_twoshot(src[i], dst, count, flags=flags)
+        nb.nuna_expert_combine(dst[n - 1], row, seen[i], tokens, 1, tokens, hidden, flags=flags)
+
+    def steps():
+        for _ in range(4):
+            look(0), reduce(0), reduce(1), look(1)
+
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        steps()
+    for run in (steps, g.replay):
+        src[0][0][:head] = src[1][0][:head] = 5.0                      # written by the lookups, for the second of them in a pass before
+        for d in dst + seen:
+            d.fill_(7.0)
+        run(), run(), run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(d, want[1]) for d in dst)
+        assert all(torch.equal(s.reshape(-1), w[:head]) for s, w in zip(seen, want))
+    assert nb.nuna_device_status() == nb.NUNA_OK

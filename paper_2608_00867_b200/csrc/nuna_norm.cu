@@ -47,12 +47,30 @@ __device__ __forceinline__ void group_sum(float (&v)[N], unsigned warps, unsigne
     warp_sum<N>(v);
 }
 
-// sum / count.  The reciprocal's rounding is taken back by the remainder, so that equal elements have themselves as their mean.
+// sum / count.  The reciprocal's rounding is taken back by the remainder, so that equal elements whose sum is exact have
+// themselves as their mean.
 __device__ __forceinline__ float quotient(float sum, float count, float inverse)
 {
     const float q = sum * inverse;
     const float better = fmaf(fmaf(-q, count, sum), inverse, q);
     return isfinite(q) ? better : q;
+}
+
+// The mean of a long sum has been rounded many times over.  Where elements are as fine as the sum itself (binary32 rows; rows of
+// any length), and a row lies far from zero for its spread, that error counts in the differences from it: of 8192 equal elements of
+// 1e5, 0.98 came out where 0 is right.  Such rows have their differences, which are exact, added too: their mean belongs to
+// the mean and off the differences, its square off the variance.  It is at most n * 2^-24 * (|mean| + spread) with n (42 up to 32768
+// elements) additions in a row, so rows within 8 spreads of zero, which are left as they are, are off by 2e-5 of a spread at
+// most.  (16-bit elements of rows that a block holds: the sums of equal ones are exact, and one step of a few elements is far
+// above the mean's error.)  Where the squares overflow the mean alone is settled, if its row is finite.
+__device__ __forceinline__ bool far_from_zero(float mean, float variance) { return variance < mean * mean * 0.015625f || isinf(variance); }
+__device__ __forceinline__ float settle(float& mean, float& variance, float differences, float count, float inverse)
+{
+    float shift = quotient(differences, count, inverse);
+    if (!isfinite(shift)) shift = 0.0f;
+    mean += shift;
+    variance = fmaxf(fmaf(-shift, shift, variance), 0.0f);
+    return shift;
 }
 
 // How rows are cut.  Whole vectors: a thread's are 32 apart, a warp's consecutive.  Otherwise pairs of elements that are 32
@@ -187,8 +205,8 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
     extern __shared__ uint4 ring[];
     const unsigned warps = a.group / 32u, g = threadIdx.x / a.group, lane = threadIdx.x % a.group, groups = blockDim.x / a.group;
     const unsigned first = C::first(lane, kPacks), left = a.units > first ? a.units - first : 0u;
-    const unsigned long long step = (unsigned long long)gridDim.x * groups;
-    unsigned long long row = (unsigned long long)blockIdx.x * groups + g;
+    const unsigned step = gridDim.x * groups;                        // far below 2^31, as is the number of rows
+    unsigned row = blockIdx.x * groups + g;
     RowFetch<DT, kPacks, kVec, 2, kDepth> fetch = {{a.x, a.residual}, {a.x_stride, a.residual_stride}, {true, a.residual != nullptr},
                                                    a.rows, first, smem_u32(ring + threadIdx.x / 32u * 32u * RowFetch<DT, kPacks, kVec, 2, kDepth>::kSlots + threadIdx.x % 32u), {}};
     pdl_begin(a.rows <= step);
@@ -205,7 +223,7 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
     }
     unsigned turn = 0, stage = 0;
     const auto work = [&](unsigned left) {
-        for (unsigned long long base = (unsigned long long)blockIdx.x * groups; base < a.rows; base += step, row += step) {
+        for (unsigned base = blockIdx.x * groups; base < a.rows; base += step, row += step) {
             const bool live = row < a.rows;
             V f[kPacks][P];
             if constexpr (kVec) {
@@ -236,7 +254,7 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
             float sum[1] = {total(part)};
             group_sum<1>(sum, warps, g, red[turn]);
             turn ^= 1u;
-            const float mean = quotient(sum[0], a.count, a.inverse);
+            float mean = quotient(sum[0], a.count, a.inverse);
             part = all<V>(0.0f);
     #pragma unroll
             for (int k = 0; k < kPacks; ++k)
@@ -250,7 +268,25 @@ __global__ void __launch_bounds__(norm_threads(kPacks, kVec)) k_norm_forward(con
             float sq[1] = {total(part)};
             group_sum<1>(sq, warps, g, red[turn]);
             turn ^= 1u;
-            const float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps));
+            float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps)), variance = sq[0] * a.inverse;
+            if (DT == kF32 && far_from_zero(mean, variance)) {           // the same for the whole group
+                part = all<V>(0.0f);
+    #pragma unroll
+                for (int k = 0; k < kPacks; ++k)
+                    if (C::has(left, k))
+    #pragma unroll
+                        for (int e = 0; e < P; ++e) part = part + f[k][e];
+                float differences[1] = {total(part)};
+                group_sum<1>(differences, warps, g, red[turn]);
+                turn ^= 1u;
+                const float shift = settle(mean, variance, differences[0], a.count, a.inverse);
+                rstd = rsqrtf(variance + a.eps);
+    #pragma unroll
+                for (int k = 0; k < kPacks; ++k)
+                    if (C::has(left, k))
+    #pragma unroll
+                        for (int e = 0; e < P; ++e) f[k][e] = f[k][e] + all<V>(-shift);
+            }
             if (live && lane == 0u) {
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
@@ -280,7 +316,7 @@ template <int DT, int PT, bool kVec>
 __global__ void __launch_bounds__(1024) k_norm_forward_long(const Padded<NormArgs> a)
 {
     constexpr int E = Pack<DT, kVec>::kElems;
-    __shared__ float red[2][32];
+    __shared__ float red[3][32];
     pdl_begin(a.rows <= gridDim.x);
     const unsigned warps = blockDim.x / 32u;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -304,17 +340,31 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(const Padded<NormArg
         }
         const void* s = a.residual ? row_at(a.summed, row, a.summed_stride) : x;         // this thread's own stores
         group_sum<1>(sum, warps, 0u, red[0]);
-        const float mean = quotient(sum[0], a.count, a.inverse);
+        float mean = quotient(sum[0], a.count, a.inverse), shift = 0.0f;
+        const float from = mean;
         float sq[1] = {0.0f};
 #pragma unroll 4
         for (unsigned i = threadIdx.x; i < a.units; i += blockDim.x) {
             float f[E];
             unpack<DT, kVec>(f, load_pack<DT, kVec>(s, i));
 #pragma unroll
-            for (int e = 0; e < E; ++e) sq[0] = fmaf(f[e] - mean, f[e] - mean, sq[0]);
+            for (int e = 0; e < E; ++e) sq[0] = fmaf(f[e] - from, f[e] - from, sq[0]);
         }
         group_sum<1>(sq, warps, 0u, red[1]);
-        const float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps));
+        float rstd = rsqrtf(fmaf(sq[0], a.inverse, a.eps)), variance = sq[0] * a.inverse;
+        if (far_from_zero(mean, variance)) {                             // the same for the whole block
+            float differences[1] = {0.0f};
+#pragma unroll 4
+            for (unsigned i = threadIdx.x; i < a.units; i += blockDim.x) {
+                float f[E];
+                unpack<DT, kVec>(f, load_pack<DT, kVec>(s, i));
+#pragma unroll
+                for (int e = 0; e < E; ++e) differences[0] += f[e] - from;
+            }
+            group_sum<1>(differences, warps, 0u, red[2]);
+            shift = settle(mean, variance, differences[0], a.count, a.inverse);
+            rstd = rsqrtf(variance + a.eps);
+        }
         if (threadIdx.x == 0u) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -326,7 +376,7 @@ __global__ void __launch_bounds__(1024) k_norm_forward_long(const Padded<NormArg
             unpack_params<PT, E>(w, load_params<PT, E>(a.weight, i, kOne<PT>));
             unpack_params<PT, E>(b, load_params<PT, E>(a.bias, i, 0u));
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = fmaf((f[e] - mean) * rstd, w[e], b[e]);
+            for (int e = 0; e < E; ++e) f[e] = fmaf((f[e] - from - shift) * rstd, w[e], b[e]);
             store_pack<DT, kVec>(row_at(a.y, row, a.y_stride), i, pack<DT, kVec>(f));
         }
     }

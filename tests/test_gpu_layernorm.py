@@ -130,6 +130,44 @@ def test_rows_that_are_constant_or_not_finite(hidden):
     assert torch.equal(clean[:2], y[[0, 5]])                          # the others are none the worse for their neighbours
 
 
+@pytest.mark.parametrize("hidden", [31, 64, 1000, 1001, 2731, 5120, 8192, 8193, 12288, 16392, 40000, 65537])
+def test_constant_rows_whose_sum_is_not_exact(hidden):
+    """Equal elements have themselves as their mean and no spread, whatever rounding did to their sum: every difference from a mean
+    that is off by a few steps is exact, equal, and a small multiple of such a step, so their sum is exact too."""
+    values = torch.tensor([12345.678, 1e5 / 3, -99999.37, 1e-3, 16777215.0, 1e30 / 7, -0.1], device="cuda")
+    rows = values.numel()
+    x = values[:, None].expand(rows, hidden).contiguous()
+    bias = normal(generator(hidden), hidden)
+    y, summed, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    f32 = dict(bias=bias, mean=mean, rstd=rstd, eps=EPS, dtype=nb.NUNA_F32, param_dtype=nb.NUNA_F32)
+    nb.nuna_layernorm_forward(x, y, rows, hidden, **f32)
+    assert torch.equal(y, bias.expand_as(y)) and torch.equal(mean, values)
+    nb.nuna_layernorm_forward(x, y, rows, hidden, residual=torch.zeros_like(x), summed=summed, **f32)
+    assert torch.equal(y, bias.expand_as(y)) and torch.equal(mean, values) and torch.equal(summed, x)
+
+
+@pytest.mark.parametrize("offset,spread", [(1e5, 0.05), (-3e4, 1e-2), (1e6, 4.0), (7777.7, 1e-3)])
+@pytest.mark.parametrize("hidden", [64, 1001, 2731, 5120, 8192, 12288, 16391, 40000])
+def test_rows_a_few_steps_of_their_mean_wide(hidden, offset, spread):
+    """Rows whose spread is that of a few steps of binary32 at their mean, against 64 bits."""
+    rows = 5
+    x = normal(generator(hidden), rows, hidden) * spread + offset
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    nb.nuna_layernorm_forward(x, y, rows, hidden, mean=mean, rstd=rstd, eps=EPS, dtype=nb.NUNA_F32, param_dtype=nb.NUNA_F32)
+    s, m, rs, xh, want = forward_reference(x, None, None, None, torch.float32)
+    n = serial(hidden)
+    # The first mean is off by d0 <= n*U*mean|s|; the differences from it are exact.  Their sum is off by n*U of their absolute values,
+    # and so is the settled mean, beside its own rounding.  The mean square m2 of the differences is var + d0^2, off by n + 6
+    # roundings; d0^2 comes off it again, with 2*d0 times the settled mean's error.  Doubled, as elsewhere.
+    d0 = n * U * s.abs().mean(-1, keepdim=True)
+    dm = 2 * n * U * ((s - m).abs().mean(-1, keepdim=True) + d0)
+    m2 = ((s - m) ** 2).mean(-1, keepdim=True) + d0 ** 2
+    rel = (2 * (n + 6) * U * m2 + 2 * d0 * dm + dm ** 2) * rs ** 2 + 4 * U
+    within(mean, m[:, 0], (dm + U * m.abs())[:, 0], (hidden, offset, "mean"))
+    within(rstd, rs[:, 0], (rel * rs)[:, 0], (hidden, offset, "rstd"))
+    within(y, want, dm * rs + xh.abs() * (rel + 4 * U) + 2 * U * want.abs(), (hidden, offset, "y"))
+
+
 def backward_reference(dy, x, mean, rstd, weight, dsummed):
     xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
     g = dy.double() if weight is None else dy.double() * weight.double()

@@ -317,12 +317,17 @@ def _own_embedding_grad(nb, s, case):
     return s["dtable"]
 
 
+def _empty_rows(s, case):
+    """The rows' map where rows may have no pair (a capacity, other ranks' experts): those are zeros then."""
+    return s["pair_of_row"] if case["capacity"] or case["local"] < case["total"] else None
+
+
 def _own_experts(nb, s, case):
     n, k, rows, hidden, code = case["tokens"], case["topk"], _row_count(case), case["hidden"], CODES[case["dtype"]]
     nb.nuna_expert_sort(s["experts"], s["row_of_pair"], s["pair_of_row"], s["offsets"], n, k, case["local"], counts=s["counts"],
                         first_expert=case["first"], capacity=case["capacity"], id_bytes=s["experts"].element_size())
     nb.nuna_expert_dispatch(s["x"], s["row_of_pair"], s["out"], n, k, rows, hidden,
-                            pair_of_row=s["pair_of_row"] if case["capacity"] else None, dtype=code)
+                            pair_of_row=_empty_rows(s, case), dtype=code)
     nb.nuna_expert_combine(s["src"], s["row_of_pair"], s["y"], n, k, rows, hidden, weights=s["weights"], dtype=code)
     return {name: s[name] for name in ("row_of_pair", "pair_of_row", "offsets", "counts", "out", "y")}
 
@@ -330,7 +335,7 @@ def _own_experts(nb, s, case):
 def _own_experts_grad(nb, s, case):
     n, k, rows, hidden, code = case["tokens"], case["topk"], _row_count(case), case["hidden"], CODES[case["dtype"]]
     nb.nuna_expert_combine_backward(s["dy"], s["src"], s["weights"], s["row_of_pair"], s["dsrc"], s["dweights"], n, k, rows, hidden,
-                                    pair_of_row=s["pair_of_row"] if case["capacity"] else None, dtype=code)
+                                    pair_of_row=_empty_rows(s, case), dtype=code)
     nb.nuna_expert_combine(s["dout"], s["row_of_pair"], s["dx"], n, k, rows, hidden, dtype=code)
     return {"dsrc": s["dsrc"], "dweights": s["dweights"], "dx": s["dx"]}
 

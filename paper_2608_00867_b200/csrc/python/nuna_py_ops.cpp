@@ -137,7 +137,8 @@ PyObject* run(Op<Args>& op, Args a, PyObject* const* args, Py_ssize_t npos, PyOb
     char* base = reinterpret_cast<char*>(&a);
     for (int i = 0; i < op.n; ++i) {
         const Field& f = op.field[i];
-        if (!given[i]) {
+        // a workspace's size is its tensor's where none is given, or None
+        if (!given[i] || (given[i] == Py_None && op.workspace_bytes && f.at == op.workspace_bytes && f.kind == kSize)) {
             if (f.required) return PyErr_Format(PyExc_TypeError, "%s() missing required argument: '%s'", op.name, f.text);
             continue;
         }
@@ -270,13 +271,13 @@ PyMethodDef g_methods[] = {
      "dtype=0, param_dtype=0, x_stride=0, residual_stride=0, summed_stride=0, y_stride=0" NUNA_TAIL},
     {"nuna_layernorm_backward", NUNA_KW(entry<&g_norm_grad>),
      "nuna_layernorm_backward(dy, x, mean, rstd, dx, rows, hidden, weight=None, dsummed=None, dweight=None, dbias=None, workspace=None, "
-     "dtype=0, param_dtype=0, dy_stride=0, x_stride=0, dsummed_stride=0, dx_stride=0, workspace_bytes=0" NUNA_TAIL},
+     "dtype=0, param_dtype=0, dy_stride=0, x_stride=0, dsummed_stride=0, dx_stride=0, workspace_bytes=None" NUNA_TAIL},
     {"nuna_embedding_forward", NUNA_KW(entry<&g_lookup>),
      "nuna_embedding_forward(ids, table, out, tokens, hidden, vocab_rows, vocab_start=0, scale=1.0, dtype=0, id_bytes=8, "
      "table_stride=0, out_stride=0" NUNA_TAIL},
     {"nuna_embedding_backward", NUNA_KW(entry<&g_lookup_grad>),
      "nuna_embedding_backward(ids, dout, dtable, tokens, hidden, vocab_rows, workspace=None, vocab_start=0, scale=1.0, dtype=0, "
-     "grad_dtype=0, id_bytes=8, dout_stride=0, dtable_stride=0, workspace_bytes=0" NUNA_TAIL},
+     "grad_dtype=0, id_bytes=8, dout_stride=0, dtable_stride=0, workspace_bytes=None" NUNA_TAIL},
     {"nuna_expert_sort", NUNA_KW(entry<&g_sort>),
      "nuna_expert_sort(experts, row_of_pair, pair_of_row, offsets, tokens, topk, num_experts, counts=None, first_expert=0, capacity=0, "
      "id_bytes=8" NUNA_TAIL},

@@ -213,6 +213,20 @@ def test_arguments_by_name_and_position(name):
             f(*args[:-1], "8", **rest, stream=0)
 
 
+@pytest.mark.parametrize("name", ["nuna_layernorm_backward", "nuna_embedding_backward"])
+def test_no_size_of_a_workspace_is_none(name):
+    """The default that the documented signature has may be passed, before and after the native module took over."""
+    stand_in = nb._STAND_INS[name]
+    status(name, flags=1)
+    native = getattr(nb, name)
+    for f in (stand_in, native):
+        assert inspect.signature(f).parameters["workspace_bytes"].default is None
+        for kw, want in ((dict(hidden=0), nb.NUNA_OK), (dict(), nb.NUNA_ERR_INVALID_ARG)):       # an address has no size of its own
+            assert f(**{**OPS[name], **kw, "workspace_bytes": None}, stream=0, check=False) == want
+        with pytest.raises(TypeError):
+            f(**{**OPS[name], "hidden": None}, stream=0)
+
+
 def test_structures_match_the_header():
     """The library's own view of a call made through ctypes: field order and sizes of one of the structures."""
     class Sort(ctypes.Structure):

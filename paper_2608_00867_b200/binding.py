@@ -279,8 +279,11 @@ def nuna_allreduce_host(src, dst, count, dtype=NUNA_BF16, flags=0, two_shot=Fals
 
 
 # ---- operators around the collectives (include/nuna.h says what they compute).  Buffers are CUDA tensors of the current device
-# or addresses; a tensor whose storage is shorter than the call's sizes and strides reach is refused (NUNA_ERR_INVALID_ARG).
-# Strides are in elements, 0 for rows without gaps; workspaces are the caller's, any tensor of at least nuna_*_workspace() bytes.
+# or addresses.  Refused (NUNA_ERR_INVALID_ARG) are tensors of another element type than the call says (unsigned integers are raw
+# memory, of any type), tensors that are not contiguous and whose elements are not where the call takes them to be (rows: consecutive
+# elements, at distances that the call's stride is a multiple of), and tensors whose storage is shorter than the call's sizes and
+# strides reach.  Strides are in elements, 0 for rows without gaps; workspaces are the caller's, any tensor of at least
+# nuna_*_workspace() bytes.
 
 def nuna_layernorm_forward(x, y, rows, hidden, weight=None, bias=None, residual=None, summed=None, mean=None, rstd=None, eps=1e-5,
                            dtype=NUNA_BF16, param_dtype=NUNA_BF16, x_stride=0, residual_stride=0, summed_stride=0, y_stride=0,

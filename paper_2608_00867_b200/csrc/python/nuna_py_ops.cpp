@@ -95,8 +95,9 @@ bool right_type(const c10::TensorImpl* t, const Field& f, const char* args, int 
 }
 
 // Whether a tensor's elements are where the call takes them to be: one after the other, or in rows of consecutive elements at equal
-// distances, of which the call's distance is a multiple.  A tensor that is contiguous may stand for memory of any shape.
-bool right_place(const c10::TensorImpl* t, const Field& f, const char* args, size_t hidden)
+// distances, of which the call's distance is a multiple (one row, as the call's `bytes` tell, has none).  A tensor that is contiguous
+// may stand for memory of any shape.
+bool right_place(const c10::TensorImpl* t, const Field& f, const char* args, size_t hidden, size_t bytes)
 {
     if (t->is_contiguous() || is_raw(c10::typeMetaToScalarType(t->dtype()))) return true;
     if (!f.stride_at) return false;
@@ -109,6 +110,7 @@ bool right_place(const c10::TensorImpl* t, const Field& f, const char* args, siz
         if (sizes[d] > 1 && strides[d] != 1) return false;
         --d;
     }
+    if (bytes <= hidden * t->itemsize()) return true;
     for (; d >= 0; --d) {
         if (sizes[d] == 1) continue;
         if (next ? strides[d] != next : (strides[d] <= 0 || stride % (size_t)strides[d] != 0)) return false;
@@ -233,7 +235,7 @@ PyObject* run(Op<Args>& op, Args a, PyObject* const* args, Py_ssize_t npos, PyOb
         for (int i = 0; i < tensors && !wrong; ++i) {
             const Field& f = *held[i].field;
             if (!right_type(held[i].tensor, f, base, dtype)) wrong = " is a tensor of another type than the call says";
-            else if (!right_place(held[i].tensor, f, base, hidden)) wrong = " is a tensor whose elements are not where the call takes them to be";
+            else if (!right_place(held[i].tensor, f, base, hidden, s.v[f.span].bytes)) wrong = " is a tensor whose elements are not where the call takes them to be";
             which = f.text;
         }
     } catch (const std::exception& e) {

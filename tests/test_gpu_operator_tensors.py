@@ -121,3 +121,14 @@ def test_rows_at_the_distance_that_the_call_says():
         assert call("nuna_layernorm_forward", dict(x=view, y=y), one, x_stride=5) == nb.NUNA_OK
         assert call("nuna_layernorm_forward", dict(x=view, y=y), one) == nb.NUNA_ERR_INVALID_ARG
     torch.cuda.synchronize()
+
+
+def test_one_row_needs_no_distance():
+    wide, y = made((T, H + 8), torch.bfloat16), made((1, H), torch.bfloat16)
+    one = dict(rows=1, hidden=H, param_dtype=nb.NUNA_F32)
+    assert call("nuna_layernorm_forward", dict(x=wide[:, :H], y=y), one) == nb.NUNA_OK
+    assert call("nuna_layernorm_forward", dict(x=wide[:, :H], y=y), one, x_stride=H + 1) == nb.NUNA_OK
+    assert call("nuna_layernorm_forward", dict(x=wide[:, :2 * H:2], y=y), one) == nb.NUNA_ERR_INVALID_ARG
+    assert call("nuna_layernorm_forward", dict(x=wide.t(), y=y), one) == nb.NUNA_ERR_INVALID_ARG
+    assert call("nuna_layernorm_forward", dict(x=wide[:, :H], y=made((2, H), torch.bfloat16)), dict(one, rows=2)) == nb.NUNA_ERR_INVALID_ARG
+    torch.cuda.synchronize()

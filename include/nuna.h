@@ -425,8 +425,9 @@ int nuna_chain_destroy(void* chain);
  *    a matrix's first byte to its last, the gaps between rows included.
  *  - Sizes are at most 2^31 - 1 rows, tokens, table rows or pairs, 2^30 elements in a row and 2^46 bytes a matrix
  *    (NUNA_ERR_TOO_LARGE).  Sizes of zero are valid: outputs that a sum over nothing defines are written.
- *  - Arithmetic is binary32 whatever the element type, in an order that sizes, types and alignments decide, with
- *    one rounding at the end: the same call gives the same bits.                                               */
+ *  - Arithmetic is binary32 whatever the element type, with one rounding at the end, and the same call gives the
+ *    same bits.  The order of a sum depends on sizes, types, alignments and which optional arguments are given; in
+ *    the embedding's gradient also on the ids of the other tokens and on NUNA_GRAD_ACCUMULATE.                  */
 
 /* `flags`, bit 15: gradients of parameters (dweight, dbias, dtable) are added to what their buffers hold (in
  * binary32, rounded once) instead of replacing it.                                                           */
@@ -497,7 +498,7 @@ int nuna_embedding_forward(const nuna_embedding_t* args, unsigned flags, void* s
 /* Gradient of the lookup: dtable[v] = rne(scale * sum of dout[t] over the tokens with ids[t] = vocab_start + v);
  * every row is written, rows without a token with zeros.  With NUNA_GRAD_ACCUMULATE the sum is added to
  * dtable[v], and rows without a token are neither read nor written.  grad_dtype (of dtable): dtype or NUNA_F32.
- * The tokens are sorted by id first, so the sum's order is fixed.  workspace: nuna_embedding_workspace bytes,
+ * The tokens are sorted by id first, so the sum's order follows from the ids.  workspace: nuna_embedding_workspace bytes,
  * 32-byte aligned.                                                                                           */
 typedef struct nuna_embedding_grad {
     size_t tokens, hidden, vocab_rows;

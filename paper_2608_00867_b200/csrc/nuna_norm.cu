@@ -76,8 +76,8 @@ __device__ __forceinline__ float settle(float& mean, float& variance, float diff
 // How rows are cut.  Whole vectors: a thread's are 32 apart, a warp's consecutive.  Otherwise pairs of elements that are 32
 // apart, so that loads and stores of a warp are consecutive and sums are taken in pairs at any alignment; a thread's pairs are
 // 64 elements apart.  Either way the addresses of a row's packs differ by constants, and a warp whose packs are all in the row
-// takes a loop without a question: rows that are not whole vectors are bound by instruction issue (8000 x 2731 f16 from 67
-// instructions an element and 69.5 us to 45 and 46.8; gradient 84.4 to 59.1).
+// takes a loop without a question (8000 x 2731 f16 from 67 instructions an element and 69.5 us to 35 and 41.9; gradient 84.4 to
+// 59.0).  What rows that are not whole vectors then wait for is latency: 39 to 51 % of the issue slots, 17 to 32 % of the warps.
 template <int DT, bool kVec> struct Cut {
     static constexpr int kForm = kVec ? kVector : kPair;
     static constexpr unsigned kStep = kVec ? 32 : 64;                // in units: vectors or elements
@@ -708,8 +708,11 @@ static int forward(const nuna_layernorm_t& n, unsigned flags, void* stream)
         // Many: four vectors a thread, so that a warp's part in the sums (40 instructions) is small beside its elements, and two
         // blocks, each of which works while the other one sums (4096 x 8192 bf16 without residual 25.0 us; two vectors a
         // thread in one block 37).  With a residual it is the four streams' traffic that bounds long rows, and fewer rows at a
-        // time are ahead: one block with two vectors a thread, where its groups fill it (4096 x 8192 44.4 against 47.1 us, 8192
-        // x 4096 44.1 | 46.8; but 32768 x 1024 55 | 46.4).
+        // time are ahead: one block with two vectors a thread, where its groups fill it.  Two | four vectors a thread, us for 256
+        // MiB, groups that fill the block: bf16 3840 43.1 | 46.6, 4096 42.3 | 46.3, 8192 43.3 | 46.7, f32 4096 43.5 | 46.4, but f32 1920
+        // and 2048 48.8 | 46.4; groups that do not: bf16 5120 54.6 | 46.8, 6144 47.6 | 44.6, 7168 46.2 | 46.6, 7680 44.6 | 46.7, f32 3584
+        // 42.1 | 46.6; shorter rows: bf16 3584 44.5 | 47.0, 2048 44.9 | 46.1, 1024 55 | 46.4.  So the rule is right for the widths that it takes, but
+        // for 1920 to 2048 binary32, and leaves up to a tenth at some that it does not.
         const bool few = a.rows <= 2 * kSms;
         if (vec && (a.units <= 32 || (few && a.units <= 256))) return run(Num<1>{}, Yes{}, 256, 1024);
         if (vec && few && a.units <= 512) return run(Num<2>{}, Yes{}, 256, 1024);
@@ -717,7 +720,7 @@ static int forward(const nuna_layernorm_t& n, unsigned flags, void* stream)
         if (vec && a.residual && a.units >= 480 && a.units <= 1024 && 512u % group_for(a.units, 2) == 0u) return run(Num<2>{}, Yes{}, 512, 512);
         if (vec && a.units <= 64) return run(Num<2>{}, Yes{}, 256, 512);
         if (vec && a.units <= 2048) return run(Num<4>{}, Yes{}, 256, 512);
-        // Pairs: eight a thread, as far as registers go; f16 four (8000 x 2731 bf16 45.8 us with eight against 56.8, f16 75 | 46.9:
+        // Pairs: eight a thread, as far as registers go; f16 four (8000 x 2731 bf16 45.8 us with eight against 56.8, f16 75 | 41.9:
         // the compiler takes half as many instructions again for its eight).
         constexpr int kLong = DT == kF16 ? 4 : 8;
         if (!vec && a.units <= 1024) return run(Num<4>{}, No{}, 256, 1024);
